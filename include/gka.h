@@ -340,6 +340,102 @@ gka_status gka_forward_sketched(const gka_params *p,
                                 void *workspace, size_t workspace_bytes,
                                 void *hip_stream);
 
+/* ---- Linear attention with a decay for each head ----------------------------------------------------------------
+ * The layer's recurrence without the solve (Section 2; what stacks that mix layers run beside it, and the limit of the
+ * alpha-connection for alpha = 0): a float32 state S [d_v, d_k] for every sequence and key/value head,
+ *     S_t = gamma_t S_{t-1} + v_t k_t^T,    y_t = S_t q_t,
+ * read by the H / H_kv query heads of its group (query head h: state h / (H / H_kv)). The conventions at the top of this file
+ * hold. Gates at or below exp(-100), including 0, wipe the state (packed sequences: a gate of 0 at each first token).
+ *
+ * Tensors of rows: q [B,T,H,d_k], k [B,T,H_kv,d_k], v [B,T,H_kv,d_v], o [B,T,H,d_v], all GKA_F32 or all GKA_BF16, 16-byte
+ * aligned; each has element strides of its own. Sums, states and decays are float32 or wider for either type; with bf16
+ * tensors what is computed in float32 enters the matrix products as two or three bf16 pieces, so that an output carries the
+ * rounding of its own type. */
+typedef struct {
+    int32_t B;            /* sequences                                                                 */
+    int32_t H;            /* query heads, a multiple of H_kv                                           */
+    int32_t H_kv;         /* key/value heads = states of a sequence                                    */
+    int32_t T;            /* tokens per sequence, any T >= 1 (ignored by gka_linear_decode_shared)     */
+    int32_t d_k;          /* features of q and k: a multiple of 16 up to 256                           */
+    int32_t d_v;          /* features of v and o: likewise                                             */
+    int32_t io_dtype;     /* gka_dtype of q, k, v, o                                                   */
+    int32_t gate_per_head;/* 0: gate [B,T,H_kv] float32, packed; 1: gate [H_kv], one decay for a head  */
+    int32_t share;        /* consecutive sequences that start from one state: sequence b reads initial */
+                          /*   state (prefix) b / share; a divisor of B (0 = 1)                        */
+    int32_t cache_tokens; /* gka_linear_decode_shared: tokens N that a suffix cache has room for       */
+    int32_t walk_chunks;  /* gka_linear_forward, _backward: chunks one workgroup walks (0 = the        */
+                          /*   library's choice); results depend on it through rounding only           */
+    int32_t reserved;     /* 0                                                                         */
+    int64_t q_stride[3];  /* element strides of batch, token and head (the features of a row are       */
+    int64_t k_stride[3];  /*   contiguous): positive, multiples of 16 bytes; 0,0,0 = packed            */
+    int64_t v_stride[3];
+    int64_t o_stride[3];  /* of o, and of dy in the backward pass                                      */
+} gka_linear_params;
+
+/* Whole sequences.
+ *   S_init  [B/share,H_kv,d_v,d_k] float32 or NULL (zero); the first gate multiplies it
+ *   S_final [B,H_kv,d_v,d_k] float32, written if not NULL: the states after the last token. May be S_init's buffer unless
+ *           share > 1 (GKA_ERR_SHAPE)
+ *   o must not overlap the inputs
+ *   workspace: gka_linear_forward_workspace_bytes(p) bytes (0: p is invalid), 256-byte aligned: states and decays of the
+ *   segments that the sequences are cut into, at most 1024 of up to 128 KiB or three for each state; contents unspecified
+ *   afterwards. */
+size_t gka_linear_forward_workspace_bytes(const gka_linear_params *p);
+gka_status gka_linear_forward(const gka_linear_params *p,
+                              const void *q, const void *k, const void *v, const float *gate,
+                              void *o,
+                              const float *S_init, float *S_final,
+                              void *workspace, size_t workspace_bytes,
+                              void *hip_stream);
+
+/* Gradients of gka_linear_forward, given dy = dL/do and optionally dS_final = dL/dS_final [B,H_kv,d_v,d_k] (NULL: zero):
+ *     dS_t = sum over the group dy_t q_t^T + gamma_{t+1} dS_{t+1},   dq_t = S_t^T dy_t,  dk_t = dS_t^T v_t,  dv_t = dS_t k_t,
+ *     dgamma_t = <dS_t, S_{t-1}>,   dS_init = gamma_0 dS_0 (summed over the sequences that share a state).
+ *   dq, dk, dv  io_dtype, packed like q, k, v (written; dk and dv summed over the query heads of a group)
+ *   dgate       float32 like gate (written; [H_kv] with gate_per_head: summed over sequences and tokens). Formed as
+ *               (<dS_final,S_T> + sum_{s>=t} (q_s . dq_s - k_s . dk_s)) / gamma_t; where a gate wipes the state it is
+ *               written as 0 and the sum restarts
+ *   dS_init     [B/share,H_kv,d_v,d_k] float32, written if not NULL
+ *   Nothing is added up by atomics: results are the same on every run.
+ *   workspace: gka_linear_backward_workspace_bytes(p) bytes, 256-byte aligned. */
+size_t gka_linear_backward_workspace_bytes(const gka_linear_params *p);
+gka_status gka_linear_backward(const gka_linear_params *p,
+                               const void *q, const void *k, const void *v, const float *gate,
+                               const void *dy,
+                               const float *S_init, const float *dS_final,
+                               void *dq, void *dk, void *dv, float *dgate, float *dS_init,
+                               void *workspace, size_t workspace_bytes,
+                               void *hip_stream);
+
+/* The next T tokens (usually one) of every sequence on stored states; the states cross HBM once per call.
+ *   S_in  [B/share,H_kv,d_v,d_k] float32; S_out [B,H_kv,d_v,d_k] float32 (written): S_in's own buffer for a cache that is
+ *         updated in place (share = 1), another one where the states before are still needed or shared. No other overlap.
+ * The arithmetic is float32. For long segments gka_linear_forward (with S_init, S_final) is the faster path. */
+gka_status gka_linear_decode(const gka_linear_params *p,
+                             const float *S_in, float *S_out,
+                             const void *q, const void *k, const void *v, const float *gate,
+                             void *o, void *hip_stream);
+
+/* One token of every sequence of a batch whose sequences continue common prefixes: of a linear-attention layer a prefix is one
+ * state (gka_linear_forward's S_final), which is read as it is, once for all, and never copied. The tokens behind it lie in a
+ * cache of each sequence's own; the call adds the new token to it and reads the sequence's n + 1 tokens,
+ *     y = zeta S_prefix q + sum_j M_j (k_j . q) v_j,   M_j = gamma_{j+1} .. gamma_n,   zeta = gamma_0 .. gamma_n.
+ *   S_prefix   [B/share,H_kv,d_v,d_k] float32
+ *   q [B,H,d_k], k [B,H_kv,d_k], v [B,H_kv,d_v], o [B,H,d_v]: the new token (token strides are not used); gate [B,H_kv] or [H_kv]
+ *   k_cache [B,N,H_kv,d_k], v_cache [B,N,H_kv,d_v] io_dtype, gate_cache [B,N,H_kv] float32 (NULL with gate_per_head), packed,
+ *              N = p->cache_tokens: row lengths[b] of sequence b is written
+ *   lengths    [B] int32, DEVICE pointer: tokens in the cache before the call, 0 .. N - 1; the caller counts them up.
+ *              A sequence with another value takes no part (idle rows of a padded batch, full caches): its rows of the caches
+ *              and of o are left as they are
+ * A cache that starts out with k = 0 and gates of 1 is folded into states of the sequences' own by one gka_linear_forward over
+ * its rows with S_init = S_prefix: rows that no token has filled change nothing. That is worth it from about 2 d_k d_v / (d_k + d_v)
+ * tokens on, where a cache in bf16 has grown as large as a state that is read and written (equal d: d tokens). */
+gka_status gka_linear_decode_shared(const gka_linear_params *p,
+                                    const float *S_prefix,
+                                    const void *q, const void *k, const void *v, const float *gate,
+                                    void *k_cache, void *v_cache, float *gate_cache, const int32_t *lengths,
+                                    void *o, void *hip_stream);
+
 const char *gka_status_string(gka_status s);
 
 /* Library version: major * 10000 + minor * 100 + patch. */

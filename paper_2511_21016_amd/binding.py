@@ -33,6 +33,12 @@ EXPORTED_SYMBOLS = (
     "gka_backward_from_state",
     "gka_forward_sketched_workspace_bytes",
     "gka_forward_sketched",
+    "gka_linear_forward_workspace_bytes",
+    "gka_linear_forward",
+    "gka_linear_backward_workspace_bytes",
+    "gka_linear_backward",
+    "gka_linear_decode",
+    "gka_linear_decode_shared",
     "gka_status_string",
     "gka_version",
 )
@@ -48,6 +54,19 @@ class GkaParams(ctypes.Structure):
         ("lambda_scale", ctypes.c_float), ("state_layout", ctypes.c_int32),
         ("beta", ctypes.c_void_p), ("alpha", ctypes.c_void_p), ("xhat_out", ctypes.c_void_p),
         ("slab_state_bytes", ctypes.c_int64), ("walk_chunks", ctypes.c_int32), ("path", ctypes.c_int32),
+    ]
+
+
+_Strides = ctypes.c_int64 * 3
+
+
+class GkaLinearParams(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("T", ctypes.c_int32),
+        ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+        ("gate_per_head", ctypes.c_int32), ("share", ctypes.c_int32), ("cache_tokens", ctypes.c_int32),
+        ("walk_chunks", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("q_stride", _Strides), ("k_stride", _Strides), ("v_stride", _Strides), ("o_stride", _Strides),
     ]
 
 
@@ -103,6 +122,19 @@ def load_library():
         lib.gka_forward_sketched.argtypes = [ctypes.POINTER(GkaParams), vp, vp, vp, fp, fp, fp, ctypes.c_int,
                                              ctypes.c_int, vp, vp, ctypes.c_size_t, vp]
         lib.gka_forward_sketched.restype = ctypes.c_int
+        lp = ctypes.POINTER(GkaLinearParams)
+        lib.gka_linear_forward_workspace_bytes.argtypes = [lp]
+        lib.gka_linear_forward_workspace_bytes.restype = ctypes.c_size_t
+        lib.gka_linear_forward.argtypes = [lp, vp, vp, vp, fp, vp, fp, fp, vp, ctypes.c_size_t, vp]
+        lib.gka_linear_forward.restype = ctypes.c_int
+        lib.gka_linear_backward_workspace_bytes.argtypes = [lp]
+        lib.gka_linear_backward_workspace_bytes.restype = ctypes.c_size_t
+        lib.gka_linear_backward.argtypes = [lp, vp, vp, vp, fp, vp, fp, fp, vp, vp, vp, fp, fp, vp, ctypes.c_size_t, vp]
+        lib.gka_linear_backward.restype = ctypes.c_int
+        lib.gka_linear_decode.argtypes = [lp, fp, fp, vp, vp, vp, fp, vp, vp]
+        lib.gka_linear_decode.restype = ctypes.c_int
+        lib.gka_linear_decode_shared.argtypes = [lp, fp, vp, vp, vp, fp, vp, vp, fp, vp, vp, vp]
+        lib.gka_linear_decode_shared.restype = ctypes.c_int
         lib.gka_status_string.argtypes = [ctypes.c_int]
         lib.gka_status_string.restype = ctypes.c_char_p
         lib.gka_version.argtypes = []
@@ -376,4 +408,239 @@ def gka_forward_sketched(q, k, v, gate, lam, S, n_iter, *, beta=None, lambda_sca
     stream = _stream_of(q)
     _check(forward_sketched_raw(params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(lam), _ptr(S), d_s, per_head,
                                 _ptr(o), _ptr(workspace), workspace.numel(), stream))
+    return o
+
+
+# ---- linear attention with a decay for each head ----
+
+def make_linear_params(B, H, H_kv, T, d_k, d_v, io_dtype, gate_per_head=0, share=0, cache_tokens=0, walk_chunks=0,
+                       q_stride=(0, 0, 0), k_stride=(0, 0, 0), v_stride=(0, 0, 0), o_stride=(0, 0, 0)):
+    return GkaLinearParams(B, H, H_kv, T, d_k, d_v, io_dtype, gate_per_head, share, cache_tokens, walk_chunks, 0,
+                           _Strides(*q_stride), _Strides(*k_stride), _Strides(*v_stride), _Strides(*o_stride))
+
+
+def _byref(params):
+    return None if params is None else ctypes.byref(params)
+
+
+def linear_forward_workspace_bytes(params):
+    return int(load_library().gka_linear_forward_workspace_bytes(_byref(params)))
+
+
+def linear_backward_workspace_bytes(params):
+    return int(load_library().gka_linear_backward_workspace_bytes(_byref(params)))
+
+
+def linear_forward_raw(params, q, k, v, gate, o, S_init=None, S_final=None, workspace=None, workspace_bytes=0, stream=None):
+    """gka_linear_forward on raw device addresses (ints or None). Returns the gka_status."""
+    return int(load_library().gka_linear_forward(_byref(params), q, k, v, gate, o, S_init, S_final, workspace, workspace_bytes,
+                                                 stream))
+
+
+def linear_backward_raw(params, q, k, v, gate, dy, dq, dk, dv, dgate, S_init=None, dS_final=None, dS_init=None,
+                        workspace=None, workspace_bytes=0, stream=None):
+    return int(load_library().gka_linear_backward(_byref(params), q, k, v, gate, dy, S_init, dS_final, dq, dk, dv, dgate, dS_init,
+                                                  workspace, workspace_bytes, stream))
+
+
+def linear_decode_raw(params, S_in, S_out, q, k, v, gate, o, stream=None):
+    return int(load_library().gka_linear_decode(_byref(params), S_in, S_out, q, k, v, gate, o, stream))
+
+
+def linear_decode_shared_raw(params, S_prefix, q, k, v, gate, k_cache, v_cache, gate_cache, lengths, o, stream=None):
+    return int(load_library().gka_linear_decode_shared(_byref(params), S_prefix, q, k, v, gate, k_cache, v_cache, gate_cache,
+                                                       lengths, o, stream))
+
+
+def _row_strides(x, name):
+    """Element strides (batch, token, head) of [B, T, h, d] or [B, h, d] rows; those of dimensions of size 1, which torch leaves
+    arbitrary, as packed rows have them."""
+    shape, given = x.shape, x.stride()
+    if given[-1] != 1 and shape[-1] != 1:
+        raise ValueError(f"{name}: the features of a row must be contiguous")
+    if x.is_contiguous():
+        return (0, 0, 0)
+    packed, strides = shape[-1], []
+    for n, s in zip(shape[-2::-1], given[-2::-1]):
+        s = packed if n == 1 else s
+        strides.append(s)
+        packed = s * n
+    if len(shape) == 3:
+        strides.insert(1, strides[1])
+    return tuple(reversed(strides))
+
+
+def _linear_params(q, k, v, gate, out=None, states=None, lead=None, cache_tokens=0, walk_chunks=0):
+    """gka_linear_params of these tensors, after the checks that only the binding can make: shapes, types, devices.
+    out: the tensor with o's strides; states: (name, tensor or None, one per sequence) of further float32 states."""
+    import torch
+    lead = q.dim() if lead is None else lead
+    if q.dim() != lead or k.dim() != lead or v.dim() != lead:
+        raise ValueError(f"q, k, v: expected {lead} dimensions, got {q.dim()}, {k.dim()}, {v.dim()}")
+    H, d_k = q.shape[-2:]
+    H_kv, d_v = v.shape[-2:]
+    tokens = q.shape[:-2]
+    if k.shape != tokens + (H_kv, d_k) or v.shape[:-2] != tokens:
+        raise ValueError(f"shapes do not fit: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+    if not q.dtype == k.dtype == v.dtype:
+        raise TypeError("q, k, v must have one dtype")
+    io = _io_dtype(q)
+    per_head = gate.dim() == 1
+    if gate.shape != ((H_kv,) if per_head else tokens + (H_kv,)):
+        raise ValueError(f"gate: expected {tuple(tokens) + (H_kv,)} or {(H_kv,)}, got {tuple(gate.shape)}")
+    if gate.dtype != torch.float32 or not gate.is_contiguous():
+        raise ValueError("gate must be contiguous float32")
+    if out is not None:
+        if out.shape != tokens + (H, d_v) or out.dtype != q.dtype:
+            raise ValueError(f"expected {tuple(tokens) + (H, d_v)} {q.dtype} for the output's rows, got {tuple(out.shape)} {out.dtype}")
+    B = tokens[0]
+    share = 0
+    for name, S, shared in states or ():
+        if S is None:
+            continue
+        n = S.shape[0] if S.dim() == 4 else 0
+        if S.dim() != 4 or S.shape[1:] != (H_kv, d_v, d_k) or n < 1 or B % n or (n != B and not shared):
+            raise ValueError(f"{name}: expected states [{B}, {H_kv}, {d_v}, {d_k}]" + (" or of a divisor of the batch" if shared else ""))
+        if S.dtype != torch.float32 or not S.is_contiguous():
+            raise ValueError(f"{name} must be contiguous float32")
+        if shared:
+            share = B // n
+    device = q.get_device()
+    for x in (k, v, gate, out, *(S for _, S, _ in states or ())):
+        if x is not None and x.get_device() != device:
+            raise ValueError("all tensors must be on one device")
+    return make_linear_params(B, H, H_kv, tokens[1] if lead == 4 else 1, d_k, d_v, io, 1 if per_head else 0, share, cache_tokens,
+                              walk_chunks, _row_strides(q, "q"), _row_strides(k, "k"), _row_strides(v, "v"),
+                              (0, 0, 0) if out is None else _row_strides(out, "out"))
+
+
+class _OnDevice:
+    """Makes the tensors' device the current one, where it is another: a launch goes to the current device."""
+
+    def __init__(self, index):
+        import torch
+        self.guard = None if torch.cuda.current_device() == index else torch.cuda.device(index)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _workspace_for(nbytes, workspace, device, name_the_error):
+    import torch
+    if nbytes == 0:
+        _check(name_the_error())                   # let the library say what is wrong with the parameters
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if workspace.get_device() != device.index or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the tensors' device")
+    return workspace
+
+
+def linear_workspace(q, k, v, gate, *, backward=False, walk_chunks=0):
+    """A workspace for calls of gka_linear_forward (or gka_linear_backward) with tensors of these sizes, for programs that
+    keep one. Two calls that may run at the same time (other streams, other graphs) need one each."""
+    import torch
+    load_library()
+    _stream_of(q)
+    params = _linear_params(q, k, v, gate, lead=4, walk_chunks=walk_chunks)
+    if backward:
+        nbytes = linear_backward_workspace_bytes(params)
+    else:
+        nbytes = linear_forward_workspace_bytes(params)
+    if nbytes == 0:
+        _check(linear_forward_raw(params, None, None, None, None, None))
+    return torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+
+
+def gka_linear_forward(q, k, v, gate, *, S_init=None, return_state=False, workspace=None, out=None, S_final=None,
+                       walk_chunks=0):
+    """gka_linear_forward on torch CUDA tensors: q [B,T,H,d_k], k [B,T,H_kv,d_k], v [B,T,H_kv,d_v] (float32 or bfloat16, any
+    strides with contiguous features), gate [B,T,H_kv] float32 or [H_kv] (one decay for each head); S_init: states
+    [B,H_kv,d_v,d_k] float32 to continue from, or [B/F,..]: each is shared by F consecutive sequences. Returns o [B,T,H,d_v],
+    with return_state (or a buffer S_final for them) also the states after the last token."""
+    import torch
+    load_library()
+    stream = _stream_of(q)
+    o = torch.empty((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device) if out is None else out
+    params = _linear_params(q, k, v, gate, o, [("S_init", S_init, True), ("S_final", S_final, False)], 4, walk_chunks=walk_chunks)
+    workspace = _workspace_for(linear_forward_workspace_bytes(params), workspace, q.device,
+                               lambda: linear_forward_raw(params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(o)))
+    if S_final is None and return_state:
+        S_final = torch.empty((q.shape[0], *v.shape[2:], q.shape[-1]), dtype=torch.float32, device=q.device)
+    with _OnDevice(q.get_device()):
+        _check(linear_forward_raw(params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(o), _ptr(S_init), _ptr(S_final),
+                                  _ptr(workspace), workspace.numel() * workspace.element_size(), stream))
+    return o if S_final is None else (o, S_final)
+
+
+def gka_linear_backward(q, k, v, gate, dy, *, S_init=None, dS_final=None, workspace=None, walk_chunks=0):
+    """gka_linear_backward on torch CUDA tensors: the arguments of gka_linear_forward, dy [B,T,H,d_v] like its output and
+    dS_final [B,H_kv,d_v,d_k] the gradient at its final states. Returns a dict: dq, dk, dv in the tensors' dtype (packed),
+    dgate float32 like gate and, with S_init, dS_init like it (summed over the sequences that share a state)."""
+    import torch
+    load_library()
+    stream = _stream_of(q)
+    params = _linear_params(q, k, v, gate, dy, [("S_init", S_init, True), ("dS_final", dS_final, False)], 4, walk_chunks=walk_chunks)
+    out = {"dq": torch.empty(q.shape, dtype=q.dtype, device=q.device), "dk": torch.empty(k.shape, dtype=k.dtype, device=k.device),
+           "dv": torch.empty(v.shape, dtype=v.dtype, device=v.device), "dgate": torch.empty_like(gate)}
+    if S_init is not None:
+        out["dS_init"] = torch.empty_like(S_init)
+    grads = [_ptr(out[n]) for n in ("dq", "dk", "dv", "dgate")]
+    workspace = _workspace_for(linear_backward_workspace_bytes(params), workspace, q.device,
+                               lambda: linear_backward_raw(params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(dy), *grads))
+    with _OnDevice(q.get_device()):
+        _check(linear_backward_raw(params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(dy), *grads, _ptr(S_init), _ptr(dS_final),
+                                   _ptr(out.get("dS_init")), _ptr(workspace), workspace.numel() * workspace.element_size(), stream))
+    return out
+
+
+def gka_linear_decode(S, q, k, v, gate, *, S_out=None, out=None):
+    """gka_linear_decode on torch CUDA tensors: states S [B,H_kv,d_v,d_k] float32, updated in place unless S_out is given (S may
+    then be [B/F,..], each state shared by F consecutive sequences); one token q [B,H,d_k], k, v, gate [B,H_kv], or T of
+    them with a token dimension behind the batch as in gka_linear_forward; gate [H_kv]: one decay for each head."""
+    import torch
+    load_library()
+    stream = _stream_of(q)
+    if q.dim() not in (3, 4):
+        raise ValueError("q: expected [B, H, d_k] or [B, T, H, d_k]")
+    o = torch.empty((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device) if out is None else out
+    target = S if S_out is None else S_out
+    params = _linear_params(q, k, v, gate, o, [("S", S, S_out is not None), ("S_out", target, False)])
+    with _OnDevice(q.get_device()):
+        _check(linear_decode_raw(params, _ptr(S), _ptr(target), _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(o), stream))
+    return o
+
+
+def gka_linear_decode_shared(S_prefix, q, k, v, gate, k_cache, v_cache, gate_cache, lengths, *, out=None):
+    """gka_linear_decode_shared on torch CUDA tensors: one token q [B,H,d_k], k [B,H_kv,d_k], v [B,H_kv,d_v], gate [B,H_kv] (or
+    [H_kv], then gate_cache is None) of B sequences, B/P consecutive ones of which continue each of the P prefixes whose
+    states S_prefix [P,H_kv,d_v,d_k] are; k_cache [B,N,H_kv,d_k], v_cache [B,N,H_kv,d_v], gate_cache [B,N,H_kv]: the
+    tokens behind the prefix, lengths [B] int32 how many of them there are; row lengths[b] is filled by the call. Sequences
+    with lengths outside 0 .. N - 1 take no part: their rows of the caches and of `out` stay as they are (without `out`:
+    unspecified)."""
+    import torch
+    load_library()
+    stream = _stream_of(q)
+    o = torch.empty((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device) if out is None else out
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache: expected [B, N, H_kv, d_k]")
+    B, N = q.shape[0], k_cache.shape[1]
+    params = _linear_params(q, k, v, gate, o, [("S_prefix", S_prefix, True)], 3, cache_tokens=N)
+    if (gate_cache is None) != (gate.dim() == 1):
+        raise ValueError("gate_cache goes with gates per token")
+    for name, cache, rows, dtype in (("k_cache", k_cache, k.shape[1:], k.dtype), ("v_cache", v_cache, v.shape[1:], v.dtype),
+                                     ("gate_cache", gate_cache, gate.shape[1:], torch.float32)):
+        if cache is not None and (cache.shape != (B, N, *rows) or cache.dtype != dtype or not cache.is_contiguous()
+                                  or cache.get_device() != q.get_device()):
+            raise ValueError(f"{name}: expected contiguous {(B, N, *rows)} {dtype} on the tensors' device")
+    if lengths.shape != (B,) or lengths.dtype != torch.int32 or not lengths.is_contiguous() or lengths.get_device() != q.get_device():
+        raise ValueError(f"lengths: expected contiguous {(B,)} int32 on the tensors' device")
+    with _OnDevice(q.get_device()):
+        _check(linear_decode_shared_raw(params, _ptr(S_prefix), _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(k_cache), _ptr(v_cache),
+                                        _ptr(gate_cache), _ptr(lengths), _ptr(o), stream))
     return o

@@ -8,7 +8,10 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgka.so")
 SOURCES = ["gka_api.hip", "gka_state_pass.hip", "gka_chunk_solve.hip", "gka_solve_f32.hip", "gka_solve_wide.hip",
            "gka_fused.hip", "gka_decode.hip", "gka_backward.hip", "gka_readout.hip", "gka_reverse.hip",
-           "gka_sketch.hip", "gka_small_dim.hip"]
+           "gka_sketch.hip", "gka_small_dim.hip", "gka_linear_api.hip", "gka_linear_bf16.hip", "gka_linear_f32.hip",
+           "gka_linear_gradient.hip", "gka_linear_decode.hip"]
+# Host code of the boundary: argument validation, launch plans, workspace carving.
+API_SOURCES = ["gka_api.hip", "gka_linear_api.hip"]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed-FP32 instructions are kept out of the generated code on purpose
@@ -62,24 +65,25 @@ def sanitizer_runtime():
 
 
 def build_host_sanitized(verbose=False):
-    """A second library whose HOST code (argument validation, launch plans, workspace carving: gka_api.hip) is
+    """A second library whose HOST code (argument validation, launch plans, workspace carving: API_SOURCES) is
     compiled with AddressSanitizer and UndefinedBehaviorSanitizer; device code and the other objects are the
     regular ones. Only the CPU tests of the boundary load it; GPU sanitizers are not involved."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objs = [os.path.join(CSRC, "_build", src.replace(".hip", ".o")) for src in SOURCES]
     if not all(os.path.exists(o) for o in objs):
         build_library(verbose=verbose)
-    san_obj = os.path.join(CSRC, "_build", "gka_api.hostsan.o")
     host_flags = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
                   "-Xarch_host", "-fno-sanitize=vptr", "-Xarch_host", "-fno-sanitize-recover=all",
                   "-Xarch_host", "-fno-omit-frame-pointer", "-g"]
-    cmd = [hipcc, *HIPCC_FLAGS, *host_flags, "-c", os.path.join(CSRC, "gka_api.hip"), "-o", san_obj]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    pr = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if pr.returncode != 0:
-        raise RuntimeError("sanitized build of gka_api.hip failed:\n" + pr.stdout)
-    objs[SOURCES.index("gka_api.hip")] = san_obj
+    for src in API_SOURCES:
+        san_obj = os.path.join(CSRC, "_build", src.replace(".hip", ".hostsan.o"))
+        cmd = [hipcc, *HIPCC_FLAGS, *host_flags, "-c", os.path.join(CSRC, src), "-o", san_obj]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        pr = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if pr.returncode != 0:
+            raise RuntimeError(f"sanitized build of {src} failed:\n" + pr.stdout)
+        objs[SOURCES.index(src)] = san_obj
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-fsanitize=address", "-fsanitize=undefined",
            "-fno-sanitize=vptr", "-shared-libsan", "-o", HOST_SANITIZED_LIB, *objs]
     if verbose:

@@ -374,6 +374,27 @@ __device__ __forceinline__ float wave_inclusive_scan(float x, int /*lane*/)
     return x;
 }
 
+// Inclusive prefix sum over the wave in float64 (the DPP moves of wave_inclusive_scan on both words).
+__device__ __forceinline__ double wave_inclusive_scan_f64(double x)
+{
+    auto dpp_add = [](double v, auto ctrl, auto row_mask) {
+        const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), decltype(ctrl)::value, decltype(row_mask)::value, 0xf, false);
+        const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), decltype(ctrl)::value, decltype(row_mask)::value, 0xf, false);
+        return v + __hiloint2double(hi, lo);
+    };
+    x = dpp_add(x, std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});
+    x = dpp_add(x, std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    x = dpp_add(x, std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    x = dpp_add(x, std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    x = dpp_add(x, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+    x = dpp_add(x, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    return x;
+}
+__device__ __forceinline__ double lane63_f64(double x)
+{
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), 63), __builtin_amdgcn_readlane(__double2loint(x), 63));
+}
+
 // Value of x on a lane known at compile time or wave-uniform (no LDS crossbar involved).
 __device__ __forceinline__ float lane_value(float x, int src_lane)
 {

@@ -1,0 +1,94 @@
+// Linear attention with a decay for each head: argument blocks and launchers of its kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gka {
+
+// A tensor of rows [B, T, heads, d]: element strides of batch, token and head; the d elements of a row are contiguous.
+struct RowTensor {
+    const void *p;
+    int64_t sb, st, sh;
+};
+
+// One walk over whole sequences: y_t = S_t q_t, S_t = gate_t S_{t-1} + sum over the sources v_t k_t^T, with S [dv, dk].
+// With other tensors in the roles of q, k, v it is the forward pass and each of the three gradients (the tensors' own names
+// on the right):
+//   y   q -> q   k -> k   v -> v    forwards           dq  q -> dy  k -> v   v -> k    forwards, S transposed
+//   dv  q -> k   k -> q   v -> dy   reverse            dk  q -> v   k -> dy  v -> q    reverse, S transposed
+// A state belongs to one of the H_kv heads; n_q queries or n_src sources of a token share it (one of the two is 1).
+// reverse: token tau of the walk is token T - 1 - tau of the tensors and its gate that of token T - tau (tau = 0: 1).
+struct LinearWalkArgs {
+    RowTensor q, k, v;            // heads: H_kv n_q, H_kv n_src, H_kv n_src; features dk, dk, dv
+    RowTensor y;                  // H_kv n_q heads, dv features (written)
+    const float *gate;            // [B, T, H_kv], or [H_kv] with gate_per_head
+    int gate_per_head, reverse;
+    int B, T, Hkv, n_q, n_src;
+    int dk, dv;                   // multiples of 16 up to 256
+    const float *init;            // [B / share, H_kv, dv, dk] or nullptr (zero)
+    int share;                    // consecutive sequences with one initial state
+    int transposed;               // init, final and state_dot_with are stored [dk, dv]
+    float *final;                 // [B, H_kv, dv, dk] or nullptr: the state behind the last token
+    int final_times_gate;         // ... times the gate of the tensors' token 0 (the gradient at the initial state)
+    // what the gradient of the decays is made of (written where the pointers are not null, in the order [slices, B, H_kv, ...]):
+    RowTensor dot_with;           // like y: dot_out [slices, B, H_kv, n_q, T] = dot_with . y, y before it is rounded
+    float *dot_out;
+    const float *state_dot_with;  // [B, H_kv, dv, dk]: state_dot_out [slices, B, H_kv] = its product with the last state
+    float *state_dot_out;
+    // plan
+    int n_segs, seg_chunks;       // segments of the walk, chunks each
+    int slices;                   // of dv, a workgroup takes one
+    float *seg_states;            // [B, H_kv, slices, n_segs, slice, DK] in the kernel's order: what each segment adds, then the
+                                  // state that it starts from
+    float *seg_decay;             // [B, H_kv, n_segs]
+};
+
+// Tokens of a chunk, features of a slice and padded dk of the kernels for these sizes; floats of a segment's state.
+struct LinearShape {
+    int chunk, slice, padded_dk, slices;
+    int64_t state_floats;
+};
+LinearShape linear_shape(bool bf16, int dk, int dv);
+hipError_t launch_linear_walk(const LinearWalkArgs &a, bool bf16, hipStream_t stream);
+hipError_t launch_linear_walk_bf16(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_walk_f32(const LinearWalkArgs &a, hipStream_t stream);
+
+// dgate_t = ([state_dot] + sum_{s >= t} (q . dq - k . dk)) / gate_t, and the sum of gradients at shared initial states.
+struct LinearGateArgs {
+    const float *q_dq;            // [q_slices, B, H_kv, G, T]
+    const float *k_dk;            // [k_slices, B, H_kv, T]
+    const float *state_dot;       // [q_slices, B, H_kv] or nullptr
+    int q_slices, k_slices, G;
+    const float *gate;
+    float *dgate;                 // [B, T, H_kv], or [H_kv] with gate_per_head
+    int gate_per_head;
+    double *per_pair;             // [B, H_kv]: scratch with gate_per_head
+    int B, T, Hkv;
+};
+hipError_t launch_linear_gate(const LinearGateArgs &a, hipStream_t stream);
+hipError_t launch_linear_state_sum(const float *per_sequence, float *out, int groups, int share, int64_t state_floats,
+                                   hipStream_t stream);
+
+// T tokens of the recurrence on stored states.
+struct LinearDecodeArgs {
+    const float *S_in;            // [B / share, H_kv, dv, dk]
+    float *S_out;                 // [B, H_kv, dv, dk]; S_in's own buffer with share = 1
+    RowTensor q, k, v, y;
+    const float *gate;            // [B, T, H_kv] or [H_kv]
+    int gate_per_head, share, B, T, Hkv, G, dk, dv;
+};
+hipError_t launch_linear_decode(const LinearDecodeArgs &a, bool bf16, hipStream_t stream);
+
+// One token of sequences that continue a shared prefix.
+struct LinearSharedArgs {
+    const float *S;               // [B / share, H_kv, dv, dk]
+    RowTensor q, k, v, y;         // one token per sequence (st unused)
+    const float *gate;            // [B, H_kv] or [H_kv]
+    void *k_cache, *v_cache;      // [B, N, H_kv, dk], [B, N, H_kv, dv]
+    float *gate_cache;            // [B, N, H_kv], nullptr with gate_per_head
+    const int32_t *lengths;       // [B]
+    int gate_per_head, share, B, N, Hkv, G, dk, dv;
+};
+hipError_t launch_linear_shared(const LinearSharedArgs &a, bool bf16, hipStream_t stream);
+
+}  // namespace gka

@@ -1,0 +1,313 @@
+// Host side of the linear-attention entry points of include/gka.h: argument checks, launch plans, workspace carving.
+// No device allocation, no synchronisation, nothing kept between calls.
+#include "../../include/gka.h"
+#include "gka_kernels.hpp"
+#include "gka_linear.hpp"
+
+namespace {
+
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+// Segments are added up to this many workgroups of a walk: two on each CU.
+constexpr int64_t kWalkWorkgroups = 2 * gka::kComputeUnits;
+
+struct Sizes {
+    int share, G;
+    int64_t pairs;
+    bool bf16;
+    gka::RowTensor q, k, v, o;    // strides only
+};
+
+enum class Call { kWalk, kDecode, kShared };
+
+// Strides of one tensor [B, T, heads, d]; all zero: packed.
+gka_status row_strides(const int64_t (&given)[3], const gka_linear_params *p, int T, int heads, int d, gka::RowTensor *x)
+{
+    x->p = nullptr;
+    x->sh = d;
+    x->st = (int64_t)heads * d;
+    x->sb = (int64_t)T * heads * d;
+    if (given[0] == 0 && given[1] == 0 && given[2] == 0) return GKA_OK;
+    const int piece = p->io_dtype == GKA_BF16 ? 8 : 4;            // rows are read and written 16 bytes at a time
+    for (int64_t s : given)
+        if (s <= 0 || s % piece) return GKA_ERR_SHAPE;
+    if (heads > 1 && given[2] < d) return GKA_ERR_SHAPE;
+    x->sb = given[0];
+    x->st = given[1];
+    x->sh = given[2];
+    return GKA_OK;
+}
+
+gka_status check(const gka_linear_params *p, Call call, Sizes *s)
+{
+    if (!p) return GKA_ERR_NULL;
+    if (p->B <= 0 || p->H <= 0 || p->H_kv <= 0 || p->H % p->H_kv) return GKA_ERR_SHAPE;
+    if (call != Call::kShared && p->T <= 0) return GKA_ERR_SHAPE;
+    if (call == Call::kShared && p->cache_tokens <= 0) return GKA_ERR_SHAPE;
+    if (p->d_k <= 0 || p->d_v <= 0) return GKA_ERR_SHAPE;
+    if (p->d_k % 16 || p->d_v % 16 || p->d_k > 256 || p->d_v > 256) return GKA_ERR_UNSUPPORTED;
+    if (p->io_dtype != GKA_F32 && p->io_dtype != GKA_BF16) return GKA_ERR_UNSUPPORTED;
+    if (p->gate_per_head != 0 && p->gate_per_head != 1) return GKA_ERR_UNSUPPORTED;
+    if (p->share < 0 || p->walk_chunks < 0) return GKA_ERR_SHAPE;
+    s->share = p->share > 0 ? p->share : 1;
+    if (p->B % s->share) return GKA_ERR_SHAPE;
+    s->G = p->H / p->H_kv;
+    s->pairs = (int64_t)p->B * p->H_kv;
+    s->bf16 = p->io_dtype == GKA_BF16;
+    if (s->pairs > (int64_t)1 << 24 || (int64_t)p->B * p->H > (int64_t)1 << 26) return GKA_ERR_SHAPE;
+    const int T = call == Call::kShared ? 1 : p->T;
+    gka_status e = row_strides(p->q_stride, p, T, p->H, p->d_k, &s->q);
+    if (e == GKA_OK) e = row_strides(p->k_stride, p, T, p->H_kv, p->d_k, &s->k);
+    if (e == GKA_OK) e = row_strides(p->v_stride, p, T, p->H_kv, p->d_v, &s->v);
+    if (e == GKA_OK) e = row_strides(p->o_stride, p, T, p->H, p->d_v, &s->o);
+    return e;
+}
+
+bool misaligned(std::initializer_list<const void *> pointers)
+{
+    for (const void *x : pointers)
+        if ((uintptr_t)x & 15) return true;
+    return false;
+}
+
+gka::RowTensor at(const void *p, gka::RowTensor strides)
+{
+    strides.p = p;
+    return strides;
+}
+
+// ---- launch plan of a walk ----
+struct WalkPlan {
+    gka::LinearShape shape;
+    int n_segs, seg_chunks;
+    size_t state_bytes, decay_bytes;   // of the segments' states and decays in the workspace
+};
+
+gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv, WalkPlan *w)
+{
+    w->shape = gka::linear_shape(s.bf16, dk, dv);
+    const int64_t chunks = ((int64_t)p->T + w->shape.chunk - 1) / w->shape.chunk;
+    const int64_t walks = s.pairs * w->shape.slices;
+    int64_t segs = 1;
+    if (p->walk_chunks > 0) {
+        segs = (chunks + p->walk_chunks - 1) / p->walk_chunks;
+        w->seg_chunks = p->walk_chunks < chunks ? p->walk_chunks : (int)chunks;
+    } else {
+        segs = (kWalkWorkgroups + walks - 1) / walks;
+        if (segs > chunks / 2) segs = chunks / 2;
+        if (segs < 1) segs = 1;
+        w->seg_chunks = (int)((chunks + segs - 1) / segs);
+    }
+    w->n_segs = (int)((chunks + w->seg_chunks - 1) / w->seg_chunks);
+    const int64_t states = walks * w->n_segs;
+    // (the scan runs state_floats / 1024 workgroups for each state of a walk)
+    if (states > 0x7fffffff || walks * (w->shape.state_floats / 1024) > 0x7fffffff) return GKA_ERR_SHAPE;
+    w->state_bytes = w->n_segs > 1 ? align_up((size_t)states * w->shape.state_floats * sizeof(float), 256) : 0;
+    w->decay_bytes = w->n_segs > 1 ? align_up((size_t)s.pairs * w->n_segs * sizeof(float), 256) : 0;
+    return GKA_OK;
+}
+
+gka::LinearWalkArgs walk_args(const gka_linear_params *p, const Sizes &s, const WalkPlan &w, const float *gate, int dk, int dv, char *ws)
+{
+    gka::LinearWalkArgs a = {};
+    a.gate = gate;
+    a.gate_per_head = p->gate_per_head;
+    a.B = p->B; a.T = p->T; a.Hkv = p->H_kv;
+    a.n_q = a.n_src = 1;
+    a.dk = dk; a.dv = dv;
+    a.share = 1;
+    a.n_segs = w.n_segs; a.seg_chunks = w.seg_chunks;
+    a.slices = w.shape.slices;
+    a.seg_states = (float *)ws;
+    a.seg_decay = (float *)(ws + w.state_bytes);
+    return a;
+}
+
+struct BackwardPlan {
+    Sizes s;
+    WalkPlan q, k, v;                  // the walks of dq, dk, dv
+    size_t off_q_dot, off_k_dot, off_state_dot, off_pair, off_states, total;
+};
+
+gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
+{
+    gka_status e = check(p, Call::kWalk, &b->s);
+    if (e != GKA_OK) return e;
+    if ((e = plan_walk(p, b->s, p->d_v, p->d_k, &b->q)) != GKA_OK) return e;
+    b->k = b->q;
+    if ((e = plan_walk(p, b->s, p->d_k, p->d_v, &b->v)) != GKA_OK) return e;
+    size_t off = 0;
+    for (const WalkPlan *w : {&b->q, &b->v})
+        if (off < w->state_bytes + w->decay_bytes) off = w->state_bytes + w->decay_bytes;
+    const size_t tokens = (size_t)b->s.pairs * p->T;
+    b->off_q_dot = off; off += align_up(b->q.shape.slices * tokens * b->s.G * sizeof(float), 256);
+    b->off_k_dot = off; off += align_up(b->k.shape.slices * tokens * sizeof(float), 256);
+    b->off_state_dot = off; off += align_up(b->q.shape.slices * b->s.pairs * sizeof(float), 256);
+    b->off_pair = off; off += align_up(b->s.pairs * sizeof(double), 256);
+    b->off_states = off;
+    // (room for a state of every sequence whether or not initial states are shared: one size for all calls)
+    off += align_up((size_t)b->s.pairs * p->d_k * p->d_v * sizeof(float), 256);
+    b->total = off;
+    return GKA_OK;
+}
+
+}  // namespace
+
+namespace gka {
+
+LinearShape linear_shape(bool bf16, int dk, int dv)
+{
+    LinearShape s;
+    s.chunk = bf16 ? 64 : 32;
+    s.slice = dv <= 64 ? 64 : 128;
+    s.padded_dk = dk <= 64 ? 64 : dk <= 128 ? 128 : 256;
+    s.slices = (dv + s.slice - 1) / s.slice;
+    s.state_floats = (int64_t)s.slice * s.padded_dk;
+    return s;
+}
+
+hipError_t launch_linear_walk(const LinearWalkArgs &a, bool bf16, hipStream_t stream)
+{
+    return bf16 ? launch_linear_walk_bf16(a, stream) : launch_linear_walk_f32(a, stream);
+}
+
+}  // namespace gka
+
+extern "C" {
+
+size_t gka_linear_forward_workspace_bytes(const gka_linear_params *p)
+{
+    Sizes s;
+    WalkPlan w;
+    if (check(p, Call::kWalk, &s) != GKA_OK || plan_walk(p, s, p->d_k, p->d_v, &w) != GKA_OK) return 0;
+    const size_t bytes = w.state_bytes + w.decay_bytes;
+    return bytes > 0 ? bytes : 256;
+}
+
+gka_status gka_linear_forward(const gka_linear_params *p, const void *q, const void *k, const void *v, const float *gate, void *o,
+                              const float *S_init, float *S_final, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    Sizes s;
+    WalkPlan w;
+    gka_status e = check(p, Call::kWalk, &s);
+    if (e != GKA_OK) return e;
+    if ((e = plan_walk(p, s, p->d_k, p->d_v, &w)) != GKA_OK) return e;
+    if (!q || !k || !v || !gate || !o) return GKA_ERR_NULL;
+    if (misaligned({q, k, v, o, S_init, S_final})) return GKA_ERR_SHAPE;
+    if (S_final && S_final == S_init && s.share > 1) return GKA_ERR_SHAPE;   // (states that other sequences still read)
+    const size_t need = w.state_bytes + w.decay_bytes;
+    if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) return GKA_ERR_WORKSPACE;
+    gka::LinearWalkArgs a = walk_args(p, s, w, gate, p->d_k, p->d_v, (char *)workspace);
+    a.q = at(q, s.q); a.k = at(k, s.k); a.v = at(v, s.v); a.y = at(o, s.o);
+    a.n_q = s.G;
+    a.init = S_init; a.share = s.share;
+    a.final = S_final;
+    return gka::launch_linear_walk(a, s.bf16, (hipStream_t)hip_stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
+}
+
+size_t gka_linear_backward_workspace_bytes(const gka_linear_params *p)
+{
+    BackwardPlan b;
+    return plan_backward(p, &b) == GKA_OK ? b.total : 0;
+}
+
+gka_status gka_linear_backward(const gka_linear_params *p, const void *q, const void *k, const void *v, const float *gate,
+                               const void *dy, const float *S_init, const float *dS_final, void *dq, void *dk, void *dv, float *dgate,
+                               float *dS_init, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    BackwardPlan b;
+    gka_status e = plan_backward(p, &b);
+    if (e != GKA_OK) return e;
+    if (!q || !k || !v || !gate || !dy || !dq || !dk || !dv || !dgate) return GKA_ERR_NULL;
+    if (misaligned({q, k, v, dy, S_init, dS_final, dq, dk, dv, dS_init})) return GKA_ERR_SHAPE;
+    if (!workspace || workspace_bytes < b.total || ((uintptr_t)workspace & 255)) return GKA_ERR_WORKSPACE;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    char *ws = (char *)workspace;
+    const Sizes &s = b.s;
+    float *q_dot = (float *)(ws + b.off_q_dot), *k_dot = (float *)(ws + b.off_k_dot), *state_dot = (float *)(ws + b.off_state_dot);
+    const int64_t none[3] = {0, 0, 0};
+    gka::RowTensor packed_q, packed_k, packed_v;
+    (void)row_strides(none, p, p->T, p->H, p->d_k, &packed_q);
+    (void)row_strides(none, p, p->T, p->H_kv, p->d_k, &packed_k);
+    (void)row_strides(none, p, p->T, p->H_kv, p->d_v, &packed_v);
+    {   // dq_t = S_t^T dy_t
+        gka::LinearWalkArgs a = walk_args(p, s, b.q, gate, p->d_v, p->d_k, ws);
+        a.q = at(dy, s.o); a.k = at(v, s.v); a.v = at(k, s.k); a.y = at(dq, packed_q);
+        a.n_q = s.G;
+        a.init = S_init; a.share = s.share; a.transposed = 1;
+        a.dot_with = at(q, s.q); a.dot_out = q_dot;
+        if (dS_final) {
+            a.state_dot_with = dS_final;
+            a.state_dot_out = state_dot;
+        }
+        if (gka::launch_linear_walk(a, s.bf16, stream) != hipSuccess) return GKA_ERR_LAUNCH;
+    }
+    {   // dk_t = dS_t^T v_t, dS_t = sum_g dy_t q_t^T + gate_{t+1} dS_{t+1}
+        gka::LinearWalkArgs a = walk_args(p, s, b.k, gate, p->d_v, p->d_k, ws);
+        a.q = at(v, s.v); a.k = at(dy, s.o); a.v = at(q, s.q); a.y = at(dk, packed_k);
+        a.n_src = s.G;
+        a.reverse = 1;
+        a.init = dS_final; a.transposed = 1;
+        a.dot_with = at(k, s.k); a.dot_out = k_dot;
+        if (gka::launch_linear_walk(a, s.bf16, stream) != hipSuccess) return GKA_ERR_LAUNCH;
+    }
+    {   // dv_t = dS_t k_t
+        gka::LinearWalkArgs a = walk_args(p, s, b.v, gate, p->d_k, p->d_v, ws);
+        a.q = at(k, s.k); a.k = at(q, s.q); a.v = at(dy, s.o); a.y = at(dv, packed_v);
+        a.n_src = s.G;
+        a.reverse = 1;
+        a.init = dS_final;
+        a.final = dS_init && s.share > 1 ? (float *)(ws + b.off_states) : dS_init;
+        a.final_times_gate = 1;
+        if (gka::launch_linear_walk(a, s.bf16, stream) != hipSuccess) return GKA_ERR_LAUNCH;
+        if (dS_init && s.share > 1 &&
+            gka::launch_linear_state_sum(a.final, dS_init, p->B / s.share, s.share, (int64_t)p->H_kv * p->d_k * p->d_v, stream) != hipSuccess)
+            return GKA_ERR_LAUNCH;
+    }
+    gka::LinearGateArgs g = {};
+    g.q_dq = q_dot; g.k_dk = k_dot; g.state_dot = dS_final ? state_dot : nullptr;
+    g.q_slices = b.q.shape.slices; g.k_slices = b.k.shape.slices; g.G = s.G;
+    g.gate = gate; g.dgate = dgate; g.gate_per_head = p->gate_per_head;
+    g.per_pair = (double *)(ws + b.off_pair);
+    g.B = p->B; g.T = p->T; g.Hkv = p->H_kv;
+    return gka::launch_linear_gate(g, stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
+}
+
+gka_status gka_linear_decode(const gka_linear_params *p, const float *S_in, float *S_out, const void *q, const void *k, const void *v,
+                             const float *gate, void *o, void *hip_stream)
+{
+    Sizes s;
+    gka_status e = check(p, Call::kDecode, &s);
+    if (e != GKA_OK) return e;
+    if (!S_in || !S_out || !q || !k || !v || !gate || !o) return GKA_ERR_NULL;
+    if (misaligned({S_in, S_out, q, k, v, o})) return GKA_ERR_SHAPE;
+    if (S_in == S_out && s.share > 1) return GKA_ERR_SHAPE;
+    if (s.pairs * 64 > 0x7fffffff) return GKA_ERR_SHAPE;                     // (workgroups, 16 rows of a state or more to each)
+    gka::LinearDecodeArgs a = {};
+    a.S_in = S_in; a.S_out = S_out;
+    a.q = at(q, s.q); a.k = at(k, s.k); a.v = at(v, s.v); a.y = at(o, s.o);
+    a.gate = gate; a.gate_per_head = p->gate_per_head;
+    a.share = s.share; a.B = p->B; a.T = p->T; a.Hkv = p->H_kv; a.G = s.G; a.dk = p->d_k; a.dv = p->d_v;
+    return gka::launch_linear_decode(a, s.bf16, (hipStream_t)hip_stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
+}
+
+gka_status gka_linear_decode_shared(const gka_linear_params *p, const float *S_prefix, const void *q, const void *k, const void *v,
+                                    const float *gate, void *k_cache, void *v_cache, float *gate_cache, const int32_t *lengths, void *o,
+                                    void *hip_stream)
+{
+    Sizes s;
+    gka_status e = check(p, Call::kShared, &s);
+    if (e != GKA_OK) return e;
+    if (!S_prefix || !q || !k || !v || !gate || !k_cache || !v_cache || !lengths || !o) return GKA_ERR_NULL;
+    if (!gate_cache && !p->gate_per_head) return GKA_ERR_NULL;
+    if (misaligned({S_prefix, q, k, v, k_cache, v_cache, o})) return GKA_ERR_SHAPE;
+    gka::LinearSharedArgs a = {};
+    a.S = S_prefix;
+    a.q = at(q, s.q); a.k = at(k, s.k); a.v = at(v, s.v); a.y = at(o, s.o);
+    a.gate = gate; a.gate_per_head = p->gate_per_head;
+    a.k_cache = k_cache; a.v_cache = v_cache; a.gate_cache = p->gate_per_head ? nullptr : gate_cache; a.lengths = lengths;
+    a.share = s.share; a.B = p->B; a.N = p->cache_tokens; a.Hkv = p->H_kv; a.G = s.G; a.dk = p->d_k; a.dv = p->d_v;
+    return gka::launch_linear_shared(a, s.bf16, (hipStream_t)hip_stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,6 @@
+// The walk over whole sequences for bfloat16 tensors: products on the bf16 MFMA, 64 tokens per chunk.
+#include "gka_linear_walk.hpp"
+
+namespace gka {
+hipError_t launch_linear_walk_bf16(const LinearWalkArgs &a, hipStream_t stream) { return linear::launch_walk_any<MmaBF16>(a, stream); }
+}  // namespace gka

@@ -1,0 +1,6 @@
+// The walk over whole sequences for float32 tensors: products on the float32 MFMA, 32 tokens per chunk.
+#include "gka_linear_walk.hpp"
+
+namespace gka {
+hipError_t launch_linear_walk_f32(const LinearWalkArgs &a, hipStream_t stream) { return linear::launch_walk_any<MmaF32>(a, stream); }
+}  // namespace gka
