@@ -50,8 +50,12 @@ struct LinearShape {
 };
 LinearShape linear_shape(bool bf16, int dk, int dv);
 hipError_t launch_linear_walk(const LinearWalkArgs &a, bool bf16, hipStream_t stream);
-hipError_t launch_linear_walk_bf16(const LinearWalkArgs &a, hipStream_t stream);
-hipError_t launch_linear_walk_f32(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_walk_bf16_64(const LinearWalkArgs &a, hipStream_t stream);      // (padded_dk)
+hipError_t launch_linear_walk_bf16_128(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_walk_bf16_256(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_walk_f32_64(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_walk_f32_128(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_walk_f32_256(const LinearWalkArgs &a, hipStream_t stream);
 
 // dgate_t = ([state_dot] + sum_{s >= t} (q . dq - k . dk)) / gate_t, and the sum of gradients at shared initial states.
 struct LinearGateArgs {

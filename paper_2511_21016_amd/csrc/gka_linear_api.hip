@@ -27,11 +27,13 @@ gka_status row_strides(const int64_t (&given)[3], const gka_linear_params *p, in
     x->sh = d;
     x->st = (int64_t)heads * d;
     x->sb = (int64_t)T * heads * d;
+    if (x->st >= 1 << 23) return GKA_ERR_UNSUPPORTED;
     if (given[0] == 0 && given[1] == 0 && given[2] == 0) return GKA_OK;
     const int piece = p->io_dtype == GKA_BF16 ? 8 : 4;            // rows are read and written 16 bytes at a time
     for (int64_t s : given)
         if (s <= 0 || s % piece) return GKA_ERR_SHAPE;
-    if (heads > 1 && given[2] < d) return GKA_ERR_SHAPE;
+    if ((heads > 1 && given[2] < d) || given[1] < d) return GKA_ERR_SHAPE;
+    if (given[1] >= 1 << 23) return GKA_ERR_UNSUPPORTED;          // (a chunk's rows are addressed with 32-bit byte offsets)
     x->sb = given[0];
     x->st = given[1];
     x->sh = given[2];
@@ -168,7 +170,11 @@ LinearShape linear_shape(bool bf16, int dk, int dv)
 
 hipError_t launch_linear_walk(const LinearWalkArgs &a, bool bf16, hipStream_t stream)
 {
-    return bf16 ? launch_linear_walk_bf16(a, stream) : launch_linear_walk_f32(a, stream);
+    switch (linear_shape(bf16, a.dk, a.dv).padded_dk) {
+    case 64: return bf16 ? launch_linear_walk_bf16_64(a, stream) : launch_linear_walk_f32_64(a, stream);
+    case 128: return bf16 ? launch_linear_walk_bf16_128(a, stream) : launch_linear_walk_f32_128(a, stream);
+    default: return bf16 ? launch_linear_walk_bf16_256(a, stream) : launch_linear_walk_f32_256(a, stream);
+    }
 }
 
 }  // namespace gka

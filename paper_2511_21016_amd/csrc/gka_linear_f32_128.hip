@@ -1,0 +1,7 @@
+// The walk over whole sequences for float32 tensors: products on the float32 MFMA, 32 tokens per chunk;
+// up to 128 k-features.
+#include "gka_linear_walk.hpp"
+
+namespace gka {
+hipError_t launch_linear_walk_f32_128(const LinearWalkArgs &a, hipStream_t stream) { return linear::launch_walk_dk<MmaF32, 128>(a, stream); }
+}  // namespace gka

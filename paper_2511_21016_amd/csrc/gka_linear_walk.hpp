@@ -104,23 +104,76 @@ __device__ __forceinline__ int64_t seg_state_at(const LinearWalkArgs &a, int64_t
     return ((pair * a.slices + slice) * a.n_segs + seg) * state_floats;
 }
 
-// Element [row][col] of the state that a pair starts from (row: v-feature, col: k-feature; both may lie in the padding).
-__device__ __forceinline__ const float *state_of(const float *states, const LinearWalkArgs &a, int64_t index)
-{
-    return states + index * a.dv * a.dk;
-}
-__device__ __forceinline__ f32x4 state_run(const float *S, const LinearWalkArgs &a, int row, int col)
-{
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (row >= a.dv || col >= a.dk) return x;      // (dk is a multiple of 16: four columns are all in or all out)
-    if (!a.transposed) return *(const f32x4 *)(S + (int64_t)row * a.dk + col);
+// A caller's state [dv, dk] (or stored [dk, dv]) as a raw buffer: rows and columns of the padding read as zeros, writes to them are
+// dropped. Lane (n, g) of the wave whose first v-feature is `row0`: run(jb, q4) is its elements [32 jb + 8 q4 + 4 g ..+3][row0 + n].
+struct StateAt {
+    buffer_rsrc state;
+    int lane_offset, dk, pitch;                    // pitch: bytes from one k-feature to the next
+    bool transposed;
+    __device__ __forceinline__ StateAt(const float *states, int64_t index, const LinearWalkArgs &a, int row0, int lane)
+    {
+        const int row = row0 + (lane & 31), g = lane >> 5;
+        state = __builtin_amdgcn_make_buffer_rsrc((void *)(states + index * a.dv * a.dk), 0, a.dv * a.dk * 4, 0x00020000);
+        transposed = a.transposed != 0;
+        pitch = transposed ? 4 * a.dv : 4;
+        dk = a.dk;
+        lane_offset = row < a.dv ? row * (transposed ? 4 : 4 * a.dk) + 4 * g * pitch : (int)0x80000000;
+    }
+    // (dk is a multiple of 16: whether a run exists depends on the pair of runs alone)
+    __device__ __forceinline__ bool exists(int jb, int q4) const { return 32 * jb + 16 * (q4 >> 1) < dk; }
+    __device__ __forceinline__ f32x4 load(int jb, int q4) const
+    {
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (!exists(jb, q4)) return x;
+        const int at = lane_offset + (32 * jb + 8 * q4) * pitch;
+        if (!transposed) return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(state, at, 0, 0));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = S[(int64_t)(col + e) * a.dv + row];
-    return x;
+        for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(state, at + e * pitch, 0, 0));
+        return x;
+    }
+    __device__ __forceinline__ void store(int jb, int q4, f32x4 x) const
+    {
+        if (!exists(jb, q4)) return;
+        const int at = lane_offset + (32 * jb + 8 * q4) * pitch;
+        if (!transposed) {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), state, at, 0, 0);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[e]), state, at + e * pitch, 0, 0);
+        }
+    }
+};
+
+// One chunk's rows of one head as a raw buffer: reads of tokens and features that do not exist give zeros and writes to them are
+// dropped by the buffer's bounds, without a branch. `lane` offsets (chunk_row below) count from the first row of the buffer.
+struct ChunkRows {
+    buffer_rsrc rows;
+    int top;                                       // byte offset of the walk's first token of the chunk
+};
+// ES: bytes of an element. Rows are at most 2^23 elements apart, so that a chunk's bytes stay below 2^30.
+template <int C, int ES>
+__device__ __forceinline__ ChunkRows chunk_rows(const RowTensor &x, int b, int head, int tau0, int T, int reverse)
+{
+    const int left = T - tau0;                     // tokens of the walk from here on
+    const int count = left < C ? left : C;
+    const int lowest = reverse ? left - count : tau0;
+    const char *base = (const char *)x.p + (b * x.sb + lowest * x.st + head * x.sh) * ES;
+    const int pitch = (int)x.st * ES;
+    return {__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, count * pitch, 0x00020000), reverse ? (count - 1) * pitch : 0};
+}
+// Offset of feature `col` of the chunk's row `row` but for ChunkRows::top; far outside for a feature that does not exist. A token
+// behind the last one lies behind the buffer's end or, in reverse, at a negative offset, which counts as one of 2^31 or more.
+template <int ES>
+__device__ __forceinline__ int chunk_offset(const RowTensor &x, int row, int col, bool exists, int reverse)
+{
+    const int pitch = (int)x.st * ES;
+    return exists ? (reverse ? -row : row) * pitch + col * ES : (int)0x80000000;
 }
 
+enum Group { kOne, kQueries, kSources };           // n_q = n_src = 1; several queries; several sources of a token
+
 // PIECES: of states and masked products in the readout (float32 tensors: 1). DOT: dot_out is wanted.
-template <class MMA, int DK, int NW, int PIECES, bool DOT, bool SUMMARY>
+template <class MMA, int DK, int NW, int PIECES, bool DOT, bool SUMMARY, Group GROUP>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DK > 128 ? 1 : 2, DK > 128 ? 1 : 2)))
 void linear_walk_kernel(LinearWalkArgs a)
 {
@@ -128,7 +181,7 @@ void linear_walk_kernel(LinearWalkArgs a)
     typedef typename MMA::frag frag;
     typedef typename MMA::elem_t elem_t;
     constexpr bool BF16 = SH::BF16;
-    constexpr int C = SH::C, TB = SH::TB, NT = SH::NT, NBK = SH::NBK, E = SH::E, PK = SH::PK, PV = SH::PV, HS = MMA::HS;
+    constexpr int C = SH::C, TB = SH::TB, NT = SH::NT, NBK = SH::NBK, E = SH::E, PK = SH::PK, PV = SH::PV, HS = MMA::HS, ES = SH::ES;
     constexpr int RSQ = SH::RSQ, RSK = SH::RSK, RSV = SH::RSV;
     constexpr int VW = BF16 ? 3 : 1;               // pieces of the weighted v (they end in the float32 state)
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -150,21 +203,15 @@ void linear_walk_kernel(LinearWalkArgs a)
     const int n_chunks = (a.T + C - 1) / C;
     const int chunk_begin = seg * a.seg_chunks;
     const int chunk_end = min(chunk_begin + a.seg_chunks, n_chunks);
-    const int steps = !SUMMARY && a.n_q > a.n_src ? a.n_q : a.n_src;
+    const int steps = GROUP == kQueries ? a.n_q : GROUP == kSources ? a.n_src : 1;
     const int v0 = slice * 32 * NW;                // first feature of the slice
     const int64_t state_floats = (int64_t)32 * NW * DK;
-
-    // a row of token 0 of the walk, and what leads to the next one
-    const int64_t dir = a.reverse ? -1 : 1, first = a.reverse ? a.T - 1 : 0;
-    auto rows_of = [&](const RowTensor &x, int head) {
-        return (const elem_t *)x.p + b * x.sb + first * x.st + head * x.sh;
-    };
 
     // ---- the state that the segment starts from
     f32x16 acc[NBK];
 #pragma unroll
     for (int jb = 0; jb < NBK; ++jb) acc[jb] = zero16();
-    if (!SUMMARY) {
+    if constexpr (!SUMMARY) {
         if (a.n_segs > 1) {
             const float *s = a.seg_states + seg_state_at(a, pair, slice, seg, state_floats) + w * NBK * 1024;
 #pragma unroll
@@ -176,43 +223,44 @@ void linear_walk_kernel(LinearWalkArgs a)
                     for (int e = 0; e < 4; ++e) acc[jb][4 * q4 + e] = x[e];
                 }
         } else if (a.init) {
-            const float *S = state_of(a.init, a, (int64_t)(b / a.share) * a.Hkv + h);
+            const StateAt S(a.init, (int64_t)(b / a.share) * a.Hkv + h, a, v0 + 32 * w, lane);
 #pragma unroll
             for (int jb = 0; jb < NBK; ++jb)
 #pragma unroll
                 for (int q4 = 0; q4 < 4; ++q4) {
-                    const f32x4 x = state_run(S, a, v0 + 32 * w + n, 32 * jb + 8 * q4 + 4 * g);
+                    const f32x4 x = S.load(jb, q4);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[jb][4 * q4 + e] = x[e];
                 }
         }
     }
 
-    // ---- rows of a chunk: memory -> registers (a step ahead) -> LDS; zeros for tokens and features that do not exist
+    // ---- rows of a chunk: memory -> registers (a step ahead) -> LDS
     struct Rows {
-        u32x4_t q[PK], k[PK], v[PV];
+        u32x4_t q[SUMMARY ? 1 : PK], k[PK], v[PV];
         float gate;
     };
     constexpr int KROW = DK / E, VROW = 32 * NW / E;          // pieces of a row
     const int krow = tid / KROW, kcol = E * (tid % KROW);     // (a thread's pieces all lie in one column)
     const int vrow = tid / VROW, vcol = E * (tid % VROW);
     const bool k_in = kcol < a.dk, v_in = v0 + vcol < a.dv;
-    auto fetch_rows = [&](u32x4_t *to, const RowTensor &x, int head, int t0, int row0, int rows_per, int col, bool in, auto count) {
-        const elem_t *p = rows_of(x, head) + (t0 + row0) * (dir * x.st) + col;
+    const int q_off = chunk_offset<ES>(a.q, krow, kcol, k_in, a.reverse);
+    const int k_off = chunk_offset<ES>(a.k, krow, kcol, k_in, a.reverse);
+    const int v_off = chunk_offset<ES>(a.v, vrow, v0 + vcol, v_in, a.reverse);
+    auto fetch_rows = [&](auto &to, const RowTensor &x, int head, int tau0, int offset, int rows_per) {
+        const ChunkRows r = chunk_rows<C, ES>(x, b, head, tau0, a.T, a.reverse);
+        const int step = chunk_offset<ES>(x, rows_per, 0, true, a.reverse);
 #pragma unroll
-        for (int i = 0; i < decltype(count)::value; ++i) {
-            const bool there = in && t0 + row0 + i * rows_per < a.T;
-            to[i] = there ? *(const u32x4_t *)(p + i * rows_per * (dir * x.st)) : u32x4_t{0, 0, 0, 0};
-        }
+        for (int i = 0; i < (int)(sizeof(to) / 16); ++i)
+            to[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r.rows, offset + (r.top + i * step), 0, 0));
     };
     auto fetch = [&](Rows &f, int c, int s) {
-        const std::integral_constant<int, PK> pk;
-        const std::integral_constant<int, PV> pv;
-        if (!SUMMARY && (s == 0 || a.n_q > 1)) fetch_rows(f.q, a.q, h * a.n_q + (a.n_q > 1 ? s : 0), c * C, krow, NT / KROW, kcol, k_in, pk);
-        if (s == 0 || a.n_src > 1) {
-            const int head = h * a.n_src + (a.n_src > 1 ? s : 0);
-            fetch_rows(f.k, a.k, head, c * C, krow, NT / KROW, kcol, k_in, pk);
-            fetch_rows(f.v, a.v, head, c * C, vrow, NT / VROW, v0 + vcol, v_in, pv);
+        if constexpr (!SUMMARY)
+            if (GROUP == kQueries || s == 0) fetch_rows(f.q, a.q, GROUP == kQueries ? h * steps + s : h, c * C, q_off, NT / KROW);
+        if (GROUP == kSources || s == 0) {
+            const int head = GROUP == kSources ? h * steps + s : h;
+            fetch_rows(f.k, a.k, head, c * C, k_off, NT / KROW);
+            fetch_rows(f.v, a.v, head, c * C, v_off, NT / VROW);
         }
         if (s == 0) {
             const int tau = c * C + lane;
@@ -222,11 +270,12 @@ void linear_walk_kernel(LinearWalkArgs a)
         }
     };
     auto stage = [&](const Rows &f, int s) {
-        if (!SUMMARY && (s == 0 || a.n_q > 1)) {
+        if constexpr (!SUMMARY)
+            if (GROUP == kQueries || s == 0) {
 #pragma unroll
-            for (int i = 0; i < PK; ++i) *(u32x4_t *)(sQ + (krow + i * (NT / KROW)) * RSQ + kcol) = f.q[i];
-        }
-        if (s == 0 || a.n_src > 1) {
+                for (int i = 0; i < PK; ++i) *(u32x4_t *)(sQ + (krow + i * (NT / KROW)) * RSQ + kcol) = f.q[i];
+            }
+        if (GROUP == kSources || s == 0) {
 #pragma unroll
             for (int i = 0; i < PK; ++i) *(u32x4_t *)(sK + (krow + i * (NT / KROW)) * RSK + kcol) = f.k[i];
 #pragma unroll
@@ -242,8 +291,8 @@ void linear_walk_kernel(LinearWalkArgs a)
         const double G = wave_inclusive_scan_f64((double)log2_gate(rows.gate));
         const double Gtot = lane63_f64(G);
         const float g_hi = (float)G, g_lo = (float)(G - (double)g_hi);
-        const float zeta_C = exp2f((float)Gtot);
-        const float w_j = c * C + lane < a.T ? exp2f((float)(Gtot - G)) : 0.0f;   // of token j in the state after the chunk
+        const float zeta_C = __builtin_amdgcn_exp2f((float)Gtot);
+        const float w_j = c * C + lane < a.T ? __builtin_amdgcn_exp2f((float)(Gtot - G)) : 0.0f;   // of token j in the state after the chunk
         seg_decay *= zeta_C;
         f32x16 y[TB];
         for (int s = 0; s < steps; ++s) {
@@ -254,43 +303,38 @@ void linear_walk_kernel(LinearWalkArgs a)
                 sLo[lane] = g_lo;
                 sW[lane] = w_j;
             }
+            __builtin_amdgcn_sched_barrier(0);
             if (s + 1 < steps) fetch(rows, c, s + 1);
             else if (c + 1 < chunk_end) fetch(rows, c + 1, 0);
             lds_barrier();                         // (no wait for the rows in flight)
-
-            frag vt[TB][HS];                       // v, features on the lanes, tokens in kidx order
-#pragma unroll
-            for (int sb = 0; sb < TB; ++sb)
-#pragma unroll
-                for (int st = 0; st < HS; ++st) vt[sb][st] = col_frag(sV, RSV, 32 * w, sb, st, lane);
+            __builtin_amdgcn_sched_barrier(0);
 
             if constexpr (!SUMMARY) {
                 // ---- products K Q^T of the causal tiles (key block sb, token block tb)
                 // M[t, s] on register r of lane (n, g): token 32 tb + n, key 32 sb + kidx(r, g)
                 auto masked = [&](const f32x16 &x, int sb, int tb, float (&m)[16]) {
-                    const float hi = __shfl(g_hi, 32 * tb + n, 64), lo = __shfl(g_lo, 32 * tb + n, 64);
+                    const float hi = sHi[32 * tb + n], lo = sLo[32 * tb + n];
+                    const int t = 32 * (tb - sb) + n;          // (in the tile below the diagonal: above every key)
 #pragma unroll
                     for (int q4 = 0; q4 < 4; ++q4) {
                         const int s0 = 32 * sb + 8 * q4 + 4 * g;
                         const f32x4 h4 = *(const f32x4 *)(sHi + s0), l4 = *(const f32x4 *)(sLo + s0);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            m[4 * q4 + e] = s0 + e <= 32 * tb + n
+                            m[4 * q4 + e] = 8 * q4 + 4 * g + e <= t
                                                 ? x[4 * q4 + e] * __builtin_amdgcn_exp2f((hi - h4[e]) + (lo - l4[e]))
                                                 : 0.0f;
                     }
                 };
                 if constexpr (BF16) {
                     // a tile to a wave; masked, cut into pieces and left as operand fragments
-#pragma unroll
-                    for (int tile = 0; tile < 3; ++tile) {
-                        if (tile % NW != w) continue;
-                        const int sb = tile == 2 ? 1 : 0, tb = tile == 0 ? 0 : 1;
+                    for (int tile = w; tile < 3; tile += NW) {
+                        const int sb = tile >> 1, tb = (tile + 1) >> 1;
                         f32x16 x = zero16();
+                        const elem_t *krow_p = sK + (32 * sb + n) * RSK, *qrow_p = sQ + (32 * tb + n) * RSQ;
 #pragma unroll
                         for (int st = 0; st < NBK * HS; ++st)
-                            x = MMA::mma(row_frag(sK + (32 * sb + n) * RSK, st / HS, st % HS, g),
-                                         row_frag(sQ + (32 * tb + n) * RSQ, st / HS, st % HS, g), x);
+                            x = MMA::mma(row_frag(krow_p, st / HS, st % HS, g), row_frag(qrow_p, st / HS, st % HS, g), x);
                         float m[16];
                         masked(x, sb, tb, m);
 #pragma unroll
@@ -316,9 +360,10 @@ void linear_walk_kernel(LinearWalkArgs a)
                     for (int q4 = 0; q4 < 4; ++q4)
                         *(f32x4 *)((float *)sP + w * 1024 + q4 * 256 + 4 * lane) = f32x4{x[4 * q4], x[4 * q4 + 1], x[4 * q4 + 2], x[4 * q4 + 3]};
                 }
+                __builtin_amdgcn_sched_barrier(0);
 
                 // ---- zeta_t S_[n] q_t: the state's tiles are the A operand
-                if (s == 0 || a.n_q > 1) {
+                if (GROUP == kQueries || s == 0) {
 #pragma unroll
                     for (int tb = 0; tb < TB; ++tb) y[tb] = zero16();
 #pragma unroll
@@ -339,12 +384,22 @@ void linear_walk_kernel(LinearWalkArgs a)
                         }
 #pragma unroll
                     for (int tb = 0; tb < TB; ++tb) {
-                        const float zeta = exp2f(__shfl(g_hi, 32 * tb + n, 64));
+                        const float zeta = __builtin_amdgcn_exp2f(sHi[32 * tb + n]);
 #pragma unroll
                         for (int r = 0; r < 16; ++r) y[tb][r] *= zeta;
                     }
                 }
                 lds_barrier();                     // the masked products are there
+                __builtin_amdgcn_sched_barrier(0);
+            }
+
+            frag vt[TB][HS];                       // v, features on the lanes, tokens in kidx order
+#pragma unroll
+            for (int sb = 0; sb < TB; ++sb)
+#pragma unroll
+                for (int st = 0; st < HS; ++st) vt[sb][st] = col_frag(sV, RSV, 32 * w, sb, st, lane);
+
+            if constexpr (!SUMMARY) {
                 // ---- + sum_s v_s M[t, s] (k_s . q_t)
                 if constexpr (BF16) {
 #pragma unroll
@@ -366,29 +421,37 @@ void linear_walk_kernel(LinearWalkArgs a)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) x[4 * q4 + e] += part[e];
                         }
+                    const float hi = sHi[n], lo = sLo[n];
                     float m[16];
-                    masked(x, 0, 0, m);
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) {
+                        const f32x4 h4 = *(const f32x4 *)(sHi + 8 * q4 + 4 * g), l4 = *(const f32x4 *)(sLo + 8 * q4 + 4 * g);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            m[4 * q4 + e] = 8 * q4 + 4 * g + e <= n ? x[4 * q4 + e] * __builtin_amdgcn_exp2f((hi - h4[e]) + (lo - l4[e])) : 0.0f;
+                    }
 #pragma unroll
                     for (int st = 0; st < HS; ++st) y[0] = MMA::mma(vt[0][st], m[st], y[0]);
                 }
                 // ---- out: lane (n, g) holds features v0 + 32 w + kidx(r, g) of token 32 tb + n
-                if (a.n_q > 1 || s + 1 == steps) {
-                    const int head = h * a.n_q + (a.n_q > 1 ? s : 0);
+                if (GROUP == kQueries || s + 1 == steps) {
+                    const int head = GROUP == kQueries ? h * steps + s : h;
                     if constexpr (DOT) {
                         float *sDot = (float *)sP; // [NW][C], in place of the masked products
+                        const ChunkRows r = chunk_rows<C, ES>(a.dot_with, b, head, c * C, a.T, a.reverse);
                         lds_barrier();
 #pragma unroll
                         for (int tb = 0; tb < TB; ++tb) {
-                            const int tau = c * C + 32 * tb + n;
-                            const elem_t *row = rows_of(a.dot_with, head) + tau * (dir * a.dot_with.st) + v0 + 32 * w + 4 * g;
                             float dot = 0.0f;
 #pragma unroll
                             for (int q4 = 0; q4 < 4; ++q4) {
-                                f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-                                if (tau < a.T && v0 + 32 * w + 8 * q4 < a.dv) {
-                                    if constexpr (BF16) x = IOBF16::load4(row, 8 * q4);
-                                    else x = IOF32::load4(row, 8 * q4);
-                                }
+                                const int col = v0 + 32 * w + 8 * q4 + 4 * g;
+                                const int at = chunk_offset<ES>(a.dot_with, 32 * tb + n, col, col < a.dv, a.reverse) + r.top;
+                                f32x4 x;
+                                if constexpr (BF16)
+                                    x = IOBF16::cvt4(__builtin_bit_cast(u16x4, __builtin_amdgcn_raw_buffer_load_b64(r.rows, at, 0, 0)));
+                                else
+                                    x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r.rows, at, 0, 0));
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) dot += x[e] * y[tb][4 * q4 + e];
                             }
@@ -401,13 +464,12 @@ void linear_walk_kernel(LinearWalkArgs a)
 #pragma unroll
                             for (int i = 0; i < NW; ++i) dot += sDot[i * C + lane];
                             const int tau = c * C + lane;
-                            a.dot_out[((((int64_t)slice * n_pairs + pair) * a.n_q) + (a.n_q > 1 ? s : 0)) * a.T + (a.reverse ? a.T - 1 - tau : tau)] = dot;
+                            a.dot_out[((((int64_t)slice * n_pairs + pair) * a.n_q) + (GROUP == kQueries ? s : 0)) * a.T + (a.reverse ? a.T - 1 - tau : tau)] = dot;
                         }
                     }
+                    const ChunkRows out = chunk_rows<C, ES>(a.y, b, head, c * C, a.T, a.reverse);
 #pragma unroll
                     for (int tb = 0; tb < TB; ++tb) {
-                        const int tau = c * C + 32 * tb + n;
-                        elem_t *row = const_cast<elem_t *>(rows_of(a.y, head)) + tau * (dir * a.y.st) + v0 + 32 * w;
                         if constexpr (BF16) {
                             // (the halves of the wave exchange runs, so that a lane stores eight features at once)
                             u32x2_t x[4];
@@ -421,29 +483,32 @@ void linear_walk_kernel(LinearWalkArgs a)
                             for (int p = 0; p < 2; ++p) {
                                 const auto r0 = __builtin_amdgcn_permlane32_swap(x[2 * p][0], x[2 * p + 1][0], false, false);
                                 const auto r1 = __builtin_amdgcn_permlane32_swap(x[2 * p][1], x[2 * p + 1][1], false, false);
-                                if (tau < a.T && v0 + 32 * w + 16 * p < a.dv)
-                                    *(u32x4_t *)(row + 16 * p + 8 * g) = u32x4_t{r0[0], r1[0], r0[1], r1[1]};
+                                const int col = v0 + 32 * w + 16 * p + 8 * g;
+                                __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{r0[0], r1[0], r0[1], r1[1]}, out.rows,
+                                                                       chunk_offset<ES>(a.y, 32 * tb + n, col, col < a.dv, a.reverse) + out.top, 0, 0);
                             }
                         } else {
 #pragma unroll
-                            for (int q4 = 0; q4 < 4; ++q4)
-                                if (tau < a.T && v0 + 32 * w + 8 * q4 < a.dv)
-                                    *(f32x4 *)(row + 8 * q4 + 4 * g) =
-                                        f32x4{y[tb][4 * q4], y[tb][4 * q4 + 1], y[tb][4 * q4 + 2], y[tb][4 * q4 + 3]};
+                            for (int q4 = 0; q4 < 4; ++q4) {
+                                const int col = v0 + 32 * w + 8 * q4 + 4 * g;
+                                const f32x4 x = {y[tb][4 * q4], y[tb][4 * q4 + 1], y[tb][4 * q4 + 2], y[tb][4 * q4 + 3]};
+                                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), out.rows,
+                                                                       chunk_offset<ES>(a.y, 32 * tb + n, col, col < a.dv, a.reverse) + out.top, 0, 0);
+                            }
                         }
                     }
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
 
             // ---- S <- zeta_C S + sum_s w_s v_s k_s^T
-            const bool first_update = a.n_src > 1 ? s == 0 : s + 1 == steps;
-            if (first_update) {
+            if (GROUP == kSources ? s == 0 : s + 1 == steps) {
 #pragma unroll
                 for (int jb = 0; jb < NBK; ++jb)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[jb][r] *= zeta_C;
             }
-            if (a.n_src > 1 || s + 1 == steps) {
+            if (GROUP == kSources || s + 1 == steps) {
 #pragma unroll
                 for (int sb = 0; sb < TB; ++sb)
 #pragma unroll
@@ -485,13 +550,13 @@ void linear_walk_kernel(LinearWalkArgs a)
         if (tid == 0 && slice == 0) a.seg_decay[(int64_t)pair * a.n_segs + seg] = seg_decay;
     } else if (seg == a.n_segs - 1) {
         if (a.state_dot_out) {
-            const float *S = state_of(a.state_dot_with, a, pair);
+            const StateAt S(a.state_dot_with, pair, a, v0 + 32 * w, lane);
             float dot = 0.0f;
 #pragma unroll
             for (int jb = 0; jb < NBK; ++jb)
 #pragma unroll
                 for (int q4 = 0; q4 < 4; ++q4) {
-                    const f32x4 x = state_run(S, a, v0 + 32 * w + n, 32 * jb + 8 * q4 + 4 * g);
+                    const f32x4 x = S.load(jb, q4);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) dot += x[e] * acc[jb][4 * q4 + e];
                 }
@@ -507,27 +572,14 @@ void linear_walk_kernel(LinearWalkArgs a)
             }
         }
         if (a.final) {
-            float *S = a.final + (int64_t)pair * a.dv * a.dk;
+            const StateAt S(a.final, pair, a, v0 + 32 * w, lane);
             float scale = 1.0f;
-            if (a.final_times_gate) scale = exp2f(log2_gate(a.gate_per_head ? a.gate[h] : a.gate[(int64_t)b * a.T * a.Hkv + h]));
-            const int row = v0 + 32 * w + n;
-            if (row < a.dv) {
+            if (a.final_times_gate) scale = __builtin_amdgcn_exp2f(log2_gate(a.gate_per_head ? a.gate[h] : a.gate[(int64_t)b * a.T * a.Hkv + h]));
 #pragma unroll
-                for (int jb = 0; jb < NBK; ++jb)
+            for (int jb = 0; jb < NBK; ++jb)
 #pragma unroll
-                    for (int q4 = 0; q4 < 4; ++q4) {
-                        const int col = 32 * jb + 8 * q4 + 4 * g;
-                        if (col >= a.dk) continue;
-                        f32x4 x = {acc[jb][4 * q4], acc[jb][4 * q4 + 1], acc[jb][4 * q4 + 2], acc[jb][4 * q4 + 3]};
-                        x *= scale;
-                        if (!a.transposed) {
-                            *(f32x4 *)(S + (int64_t)row * a.dk + col) = x;
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) S[(int64_t)(col + e) * a.dv + row] = x[e];
-                        }
-                    }
-            }
+                for (int q4 = 0; q4 < 4; ++q4)
+                    S.store(jb, q4, f32x4{acc[jb][4 * q4], acc[jb][4 * q4 + 1], acc[jb][4 * q4 + 2], acc[jb][4 * q4 + 3]} * scale);
         }
     }
 }
@@ -548,8 +600,8 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(LinearWalkArgs a)
     f32x4 run = {0.0f, 0.0f, 0.0f, 0.0f};
     if (a.init) {
         const int lane = at / 4 % 64, q4 = at / 256 % 4, jb = at / 1024 % NBK, w = at / 1024 / NBK;
-        run = state_run(state_of(a.init, a, (int64_t)(b / a.share) * a.Hkv + h), a, slice * 32 * NW + 32 * w + (lane & 31),
-                        32 * jb + 8 * q4 + 4 * (lane >> 5));
+        const StateAt S(a.init, (int64_t)(b / a.share) * a.Hkv + h, a, slice * 32 * NW + 32 * __builtin_amdgcn_readfirstlane(w), lane);
+        run = S.load(__builtin_amdgcn_readfirstlane(jb), __builtin_amdgcn_readfirstlane(q4));
     }
     const float *decay = a.seg_decay + (int64_t)pair * a.n_segs;
     f32x4 next = *(const f32x4 *)s;
@@ -561,40 +613,40 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(LinearWalkArgs a)
     }
 }
 
-template <class MMA, int DK, int NW>
-hipError_t launch_walk(const LinearWalkArgs &a, hipStream_t stream)
+template <class MMA, int DK, int NW, int PIECES, bool DOT, bool SUMMARY, Group GROUP>
+hipError_t launch_kernel(const LinearWalkArgs &a, int workgroups, hipStream_t stream)
 {
     typedef Shape<MMA, DK, NW> SH;
-    constexpr int PLAIN = SH::BF16 ? 2 : 1, EXACT = SH::BF16 ? 3 : 1;
+    constexpr size_t lds = SH::lds_bytes(PIECES, SUMMARY);
     static bool raised[kMaxLdsDevices] = {};
-    hipError_t e = raise_lds_limits(raised, {{(const void *)linear_walk_kernel<MMA, DK, NW, PLAIN, false, false>, SH::lds_bytes(PLAIN, false)},
-                                             {(const void *)linear_walk_kernel<MMA, DK, NW, EXACT, true, false>, SH::lds_bytes(EXACT, false)},
-                                             {(const void *)linear_walk_kernel<MMA, DK, NW, 1, false, true>, SH::lds_bytes(1, true)}});
+    const hipError_t e = raise_lds_limits(raised, {{(const void *)linear_walk_kernel<MMA, DK, NW, PIECES, DOT, SUMMARY, GROUP>, lds}});
     if (e != hipSuccess) return e;
-    const int n = a.B * a.Hkv * a.slices;
-    if (a.n_segs > 1) {
-        hipLaunchKernelGGL((linear_walk_kernel<MMA, DK, NW, 1, false, true>), dim3(n * (a.n_segs - 1)), dim3(SH::NT), SH::lds_bytes(1, true),
-                           stream, a);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-        hipLaunchKernelGGL((linear_scan_kernel<DK, NW>), dim3(n * (32 * NW * DK / 1024)), dim3(256), 0, stream, a);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if (a.dot_out)
-        hipLaunchKernelGGL((linear_walk_kernel<MMA, DK, NW, EXACT, true, false>), dim3(n * a.n_segs), dim3(SH::NT), SH::lds_bytes(EXACT, false),
-                           stream, a);
-    else
-        hipLaunchKernelGGL((linear_walk_kernel<MMA, DK, NW, PLAIN, false, false>), dim3(n * a.n_segs), dim3(SH::NT),
-                           SH::lds_bytes(PLAIN, false), stream, a);
+    hipLaunchKernelGGL((linear_walk_kernel<MMA, DK, NW, PIECES, DOT, SUMMARY, GROUP>), dim3(workgroups), dim3(SH::NT), lds, stream, a);
     return hipGetLastError();
 }
 
-template <class MMA>
-hipError_t launch_walk_any(const LinearWalkArgs &a, hipStream_t stream)
+template <class MMA, int DK, int NW, Group GROUP>
+hipError_t launch_walk(const LinearWalkArgs &a, hipStream_t stream)
+{
+    constexpr bool BF16 = Shape<MMA, DK, NW>::BF16;
+    const int n = a.B * a.Hkv * a.slices;
+    if (a.n_segs > 1) {
+        hipError_t e = launch_kernel<MMA, DK, NW, 1, false, true, GROUP == kSources ? kSources : kOne>(a, n * (a.n_segs - 1), stream);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((linear_scan_kernel<DK, NW>), dim3(n * (32 * NW * DK / 1024)), dim3(256), 0, stream, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    return a.dot_out ? launch_kernel<MMA, DK, NW, BF16 ? 3 : 1, true, false, GROUP>(a, n * a.n_segs, stream)
+                     : launch_kernel<MMA, DK, NW, BF16 ? 2 : 1, false, false, GROUP>(a, n * a.n_segs, stream);
+}
+
+template <class MMA, int DK>
+hipError_t launch_walk_dk(const LinearWalkArgs &a, hipStream_t stream)
 {
     const bool narrow = a.dv <= 64;
-    if (a.dk <= 64) return narrow ? launch_walk<MMA, 64, 2>(a, stream) : launch_walk<MMA, 64, 4>(a, stream);
-    if (a.dk <= 128) return narrow ? launch_walk<MMA, 128, 2>(a, stream) : launch_walk<MMA, 128, 4>(a, stream);
-    return narrow ? launch_walk<MMA, 256, 2>(a, stream) : launch_walk<MMA, 256, 4>(a, stream);
+    if (a.n_q > 1) return narrow ? launch_walk<MMA, DK, 2, kQueries>(a, stream) : launch_walk<MMA, DK, 4, kQueries>(a, stream);
+    if (a.n_src > 1) return narrow ? launch_walk<MMA, DK, 2, kSources>(a, stream) : launch_walk<MMA, DK, 4, kSources>(a, stream);
+    return narrow ? launch_walk<MMA, DK, 2, kOne>(a, stream) : launch_walk<MMA, DK, 4, kOne>(a, stream);
 }
 
 }  // namespace linear
