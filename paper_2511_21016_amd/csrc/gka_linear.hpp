@@ -37,6 +37,8 @@ struct LinearWalkArgs {
     float *state_dot_out;
     // plan
     int n_segs, seg_chunks;       // segments of the walk, chunks each
+    int scanned;                  // a launch between turns what the segments add into the states that they start from (else each
+                                  // segment adds up those before it)
     int slices;                   // of dv, a workgroup takes one
     float *seg_states;            // [B, H_kv, slices, n_segs, slice, DK] in the kernel's order: what each segment adds, then the
                                   // state that it starts from

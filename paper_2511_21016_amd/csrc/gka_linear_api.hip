@@ -11,6 +11,9 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // Segments are added up to this many workgroups of a walk: two on each CU.
 constexpr int64_t kWalkWorkgroups = 2 * gka::kComputeUnits;
 
+// Up to this many segments a walk adds up the states of those before it by itself; above, a launch between does.
+constexpr int kMostSegmentsAddedUp = 16;
+
 struct Sizes {
     int share, G;
     int64_t pairs;
@@ -119,6 +122,7 @@ gka::LinearWalkArgs walk_args(const gka_linear_params *p, const Sizes &s, const 
     a.dk = dk; a.dv = dv;
     a.share = 1;
     a.n_segs = w.n_segs; a.seg_chunks = w.seg_chunks;
+    a.scanned = w.n_segs > kMostSegmentsAddedUp;
     a.slices = w.shape.slices;
     a.seg_states = (float *)ws;
     a.seg_decay = (float *)(ws + w.state_bytes);

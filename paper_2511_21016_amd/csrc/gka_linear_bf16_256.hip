@@ -3,5 +3,5 @@
 #include "gka_linear_walk.hpp"
 
 namespace gka {
-hipError_t launch_linear_walk_bf16_256(const LinearWalkArgs &a, hipStream_t stream) { return linear::launch_walk_dk<MmaBF16, 256>(a, stream); }
+hipError_t launch_linear_walk_bf16_256(const LinearWalkArgs &a, hipStream_t stream) { return linear::launch_walk_dk<linear::Tile16BF16, 256>(a, stream); }
 }  // namespace gka

@@ -3,5 +3,5 @@
 #include "gka_linear_walk.hpp"
 
 namespace gka {
-hipError_t launch_linear_walk_f32_64(const LinearWalkArgs &a, hipStream_t stream) { return linear::launch_walk_dk<MmaF32, 64>(a, stream); }
+hipError_t launch_linear_walk_f32_64(const LinearWalkArgs &a, hipStream_t stream) { return linear::launch_walk_dk<linear::Tile16F32, 64>(a, stream); }
 }  // namespace gka

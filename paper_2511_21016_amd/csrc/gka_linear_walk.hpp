@@ -5,14 +5,18 @@
 // The same walk with other tensors in the roles of q, k, v gives the three gradients (LinearWalkArgs).
 //
 // A workgroup walks the chunks of one segment of one (sequence, kv head), for a slice of up to 128 of the dv features, with the
-// state in registers: wave w holds features 32 w .. 32 w + 31 of the slice for all k-features, accumulator tile jb element
-// [32 jb + kidx(r, g)][32 w + n] on lane (n, g), register r. A tile converts in place into the A operand of S q. Segments
-// start from states that a summary launch (SUMMARY: the updates alone) and a scan over the segments leave in the workspace.
+// state in registers. Everything is built from 16 x 16 MFMA tiles: lane 16 kg + n of an accumulator holds rows 4 kg + r (r = 0..3)
+// of column n. Wave w holds v-features 16 w .. + 15 of the slice for all k-features: tile j is S^T's rows (k-features) 16 j .. and
+// columns (v-features) 16 w ... Two tiles convert in place into one A operand of S q, whose contraction index is then
+// enumerated 4 kg .. + 3, 16 + 4 kg .. + 3 within each 32 (bf16; float32: tile by tile); q rows lie in LDS in that order, and
+// the masked products of two key tiles are an operand of the product with v without leaving their lanes. Few registers a wave
+// (128: four waves on a SIMD) matter more here than operand reuse: a chunk is a chain of short phases with barriers between.
+// Segments start from states that a summary launch (SUMMARY: the updates alone) leaves in the workspace.
 //
 // Precision. bf16 tensors enter the products as they are; what is computed in float32 (states, masked products, weighted
 // v) is cut into bf16 pieces of 8 bits each: two where the product ends in a bf16 output (17 bits against the output's 8), three
-// where it ends in float32: in the state itself, and in the dot products behind the gradient of the decays, a long sum of
-// differences. float32 tensors use the float32 MFMA. Decays are summed in float64 and kept as two floats: a difference of
+// where it ends in float32: in a state that is asked for, and in the dot products behind the gradient of the decays, a long sum
+// of differences. float32 tensors use the float32 MFMA. Decays are summed in float64 and kept as two floats: a difference of
 // two of them is then exact to float32 wherever a sequence is wiped by a gate of 0 (2^-144 each) before.
 #pragma once
 #include "gka_device.hpp"
@@ -24,117 +28,158 @@ namespace linear {
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
-// MMA: MmaBF16 (64 tokens per chunk) or MmaF32 (32). DK: padded features of q and k. NW: waves, 32 features of v each.
-template <class MMA, int DK, int NW>
-struct Shape {
-    static constexpr bool BF16 = MMA::VEC == 8;
-    static constexpr int TB = BF16 ? 2 : 1;        // 32-token blocks
-    static constexpr int C = 32 * TB;
-    static constexpr int NT = 64 * NW;
-    static constexpr int NBK = DK / 32;
-    static constexpr int E = BF16 ? 8 : 4;         // elements of a 16-byte piece
-    static constexpr int RSQ = DK + (BF16 ? 8 : 4);
-    static constexpr int RSK = DK + (BF16 ? 16 : 4);
-    static constexpr int RSV = 32 * NW + (BF16 ? 16 : 4);
-    static constexpr int PK = C * DK / E / NT;     // 16-byte pieces of a chunk's q or k rows per thread
-    static constexpr int PV = C * 32 / E / 64;     // ... of its v rows
-    static constexpr int TILES = TB == 2 ? 3 : 1;  // causal 32 x 32 tiles of the masked products
-    static constexpr int ES = sizeof(typename MMA::elem_t);
-    static constexpr size_t q_bytes = (size_t)C * RSQ * ES, k_bytes = (size_t)C * RSK * ES, v_bytes = (size_t)C * RSV * ES;
-    // masked products: bf16 fragments of up to three pieces; float32: what each wave adds to the one tile
-    static constexpr size_t p_bytes(int pieces) { return BF16 ? (size_t)TILES * 2 * 64 * 16 * pieces : (size_t)NW * 1024 * 4; }
-    static constexpr size_t tab_bytes = 3 * 64 * sizeof(float);
-    static constexpr size_t lds_bytes(int pieces, bool summary)
-    {
-        return (summary ? 0 : q_bytes + p_bytes(pieces)) + k_bytes + v_bytes + tab_bytes;
+// Products of 16 x 16 tiles. STEPS: MFMAs for a contraction over 32; VEC: operand elements per lane of each.
+struct Tile16BF16 {
+    static constexpr bool BF16 = true;
+    static constexpr int VEC = 8, STEPS = 1;
+    typedef bf16x8 frag;
+    typedef uint16_t elem_t;
+    static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ frag pack(const float *x) { return MmaBF16::pack(x); }
+    static __device__ __forceinline__ void unpack(frag f, float *x) { MmaBF16::unpack(f, x); }
+};
+struct Tile16F32 {
+    static constexpr bool BF16 = false;
+    static constexpr int VEC = 1, STEPS = 8;
+    typedef float frag;
+    typedef float elem_t;
+    static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ frag pack(const float *x) { return x[0]; }
+    static __device__ __forceinline__ void unpack(frag f, float *x) { x[0] = f; }
+};
+
+// Row-major LDS tile, D elements a row and padding such that the lanes of a read fall into different banks: 16 bytes for reads
+// of 16 rows at one 16-byte piece (and, float32, of 16 columns of 4 rows that are 4 apart), 32 for bf16 transpose reads, 32
+// bytes of 8 rows. Everything but a lane's own base is an offset known when compiling.
+template <int D, int ES, int PAD>
+struct Tile {
+    static constexpr int ROW = D * ES + PAD;
+    // byte offset of 16-byte piece `piece` of row `row`
+    static __device__ __forceinline__ int at(int row, int piece) { return row * ROW + piece * 16; }
+};
+
+// Fragments of step `st` of the contraction over a 32-block `blk`. Rows of q: its LDS tile holds the features of each 32 in the
+// order of the operands (bf16: piece kg of the block is features 4 kg .. + 3 and 16 + 4 kg .. + 3) ...
+template <class M, class T>
+__device__ __forceinline__ typename M::frag q_frag(const unsigned char *tile, int row, int blk, int st, int kg)
+{
+    if constexpr (M::BF16) return __builtin_bit_cast(bf16x8, *(const u32x4_t *)(tile + T::at(row, 4 * blk + kg)));
+    else return (*(const f32x4 *)(tile + T::at(row, 8 * blk + 4 * (st >> 2) + kg)))[st & 3];
+}
+// ... rows of k: theirs lie in natural order, for the transpose reads ...
+template <class M, class T>
+__device__ __forceinline__ typename M::frag k_row_frag(const unsigned char *tile, int row, int blk, int st, int kg)
+{
+    if constexpr (M::BF16) {
+        const u32x2_t a = *(const u32x2_t *)(tile + T::at(row, 4 * blk + (kg >> 1)) + 8 * (kg & 1));
+        const u32x2_t b = *(const u32x2_t *)(tile + T::at(row, 4 * blk + 2 + (kg >> 1)) + 8 * (kg & 1));
+        const u32x4_t u = {a[0], a[1], b[0], b[1]};
+        return __builtin_bit_cast(bf16x8, u);
+    } else {
+        return q_frag<M, T>(tile, row, blk, st, kg);
     }
-};
-
-struct RowsAt {
-    int rs;
-    __device__ __forceinline__ int operator()(int row, int col) const { return row * rs + col; }
-};
-
-// Operand fragment of step `st` of 32-feature block `blk`: a row of a row-major tile, its features in kidx order ...
-__device__ __forceinline__ bf16x8 row_frag(const uint16_t *row, int blk, int st, int g)
-{
-    const uint16_t *p = row + 32 * blk + 16 * st + 4 * g;
-    const u32x2_t a = *(const u32x2_t *)p, b = *(const u32x2_t *)(p + 8);
-    const u32x4_t u = {a[0], a[1], b[0], b[1]};
-    return __builtin_bit_cast(bf16x8, u);
 }
-__device__ __forceinline__ float row_frag(const float *row, int blk, int st, int g)
+// ... and columns 16 c16 .. + 15, contraction over the 32 rows (tokens) of block `blk`.
+template <class M, class T>
+__device__ __forceinline__ typename M::frag col_frag(const unsigned char *tile, int c16, int blk, int st, int lane)
 {
-    const f32x4 x = *(const f32x4 *)(row + 32 * blk + 8 * (st >> 2) + 4 * g);
-    return x[st & 3];
-}
-// ... or its columns col0 .. col0 + 31, the rows (tokens) of 32-block `blk` in kidx order.
-__device__ __forceinline__ bf16x8 col_frag(const uint16_t *tile, int rs, int col0, int blk, int st, int lane)
-{
-    const int t0 = 32 * blk + 16 * st + 4 * (lane >> 5);
-    return gather_transposed_bf16(tile, RowsAt{rs}, col0 + 16 * ((lane >> 4) & 1), lane, t0, t0 + 8);
-}
-__device__ __forceinline__ float col_frag(const float *tile, int rs, int col0, int blk, int st, int lane)
-{
-    return tile[(32 * blk + kidx(st, lane >> 5)) * rs + col0 + (lane & 31)];
+    const int kg = lane >> 4, i = lane & 15;
+    if constexpr (M::BF16) {
+        // (within 16 lanes, lane i supplies the address of row i / 4 at columns 4 (i % 4) .. and receives four rows of its own column)
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const int row = 32 * blk + 4 * kg + (i >> 2);
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + T::at(row, 2 * c16 + (i >> 1 & 1)) + 8 * (i & 1)));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + T::at(row + 16, 2 * c16 + (i >> 1 & 1)) + 8 * (i & 1)));
+        const s16x8 r = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        return __builtin_bit_cast(bf16x8, r);
+    } else {
+        const int row = 32 * blk + 16 * (st >> 2) + 4 * kg + (st & 3);
+        return *(const float *)(tile + T::at(row, 4 * c16 + (i >> 2)) + 4 * (i & 3));
+    }
 }
 
 // VEC floats as pieces of operand precision; all of them together hold 8 bits per piece (float32 operands: one piece, exact).
-template <class MMA, int N>
-__device__ __forceinline__ void cut(const float *x, typename MMA::frag (&f)[N])
+template <class M, int N>
+__device__ __forceinline__ void cut(const float *x, typename M::frag (&f)[N])
 {
-    float rest[MMA::VEC];
+    float rest[M::VEC];
 #pragma unroll
-    for (int e = 0; e < MMA::VEC; ++e) rest[e] = x[e];
+    for (int e = 0; e < M::VEC; ++e) rest[e] = x[e];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        f[i] = MMA::pack(rest);
+        f[i] = M::pack(rest);
         if (i + 1 < N) {
-            float back[MMA::VEC];
-            MMA::unpack(f[i], back);
+            float back[M::VEC];
+            M::unpack(f[i], back);
 #pragma unroll
-            for (int e = 0; e < MMA::VEC; ++e) rest[e] -= back[e];
+            for (int e = 0; e < M::VEC; ++e) rest[e] -= back[e];
         }
     }
 }
 
-// Float `i` of the state of segment `seg` of (pair, slice), as the scan and the walks address it: tile (w, jb), register r, lane.
+// DK: padded features of q and k. NW: waves, 16 features of v each.
+template <class M, int DK, int NW>
+struct Shape {
+    static constexpr int ES = sizeof(typename M::elem_t);
+    static constexpr int C = M::BF16 ? 64 : 32;    // tokens of a chunk
+    static constexpr int TB = C / 16, SB = C / 32; // blocks of 16 tokens, of 32 keys
+    static constexpr int NT = 64 * NW, NJ = DK / 16, KB = DK / 32;
+    static constexpr int E = 16 / ES;              // elements of a 16-byte piece
+    static constexpr int PK = (C * DK / E + NT - 1) / NT;     // pieces of a chunk's q or k rows per thread
+    static constexpr int PV = C * 16 / E / 64;     // ... of its v rows
+    static constexpr int UNITS = M::BF16 ? 6 : 2;  // (token block, 32 keys at or before it)
+    typedef Tile<DK, ES, 16> QT;
+    typedef Tile<DK, ES, M::BF16 ? 32 : 16> KT;
+    typedef Tile<16 * NW, ES, M::BF16 ? 32 : 16> VT;
+    static constexpr size_t q_bytes = (size_t)C * QT::ROW, k_bytes = (size_t)C * KT::ROW, v_bytes = (size_t)C * VT::ROW;
+    static constexpr size_t unit_bytes = M::STEPS * 64 * sizeof(typename M::frag);
+    static constexpr size_t tables = 2 * 5 * 64 * sizeof(float);
+    static constexpr size_t dot_bytes = (size_t)NW * C * sizeof(float);
+    static constexpr size_t p_bytes(int pieces) { return UNITS * unit_bytes * pieces > dot_bytes ? UNITS * unit_bytes * pieces : dot_bytes; }
+    static constexpr size_t lds_bytes(int pieces, bool summary)
+    {
+        return k_bytes + v_bytes + tables + (summary ? 0 : q_bytes + p_bytes(pieces));
+    }
+    static_assert((C * DK / E) % NT == 0 && NT % (DK / E) == 0, "a thread's pieces lie in one column");
+};
+
 __device__ __forceinline__ int64_t seg_state_at(const LinearWalkArgs &a, int64_t pair, int slice, int seg, int64_t state_floats)
 {
     return ((pair * a.slices + slice) * a.n_segs + seg) * state_floats;
 }
 
 // A caller's state [dv, dk] (or stored [dk, dv]) as a raw buffer: rows and columns of the padding read as zeros, writes to them are
-// dropped. Lane (n, g) of the wave whose first v-feature is `row0`: run(jb, q4) is its elements [32 jb + 8 q4 + 4 g ..+3][row0 + n].
+// dropped. Lane 16 kg + n of the wave whose first v-feature is `row0`: run j is its elements [16 j + 4 kg .. + 3][row0 + n].
 struct StateAt {
     buffer_rsrc state;
     int lane_offset, dk, pitch;                    // pitch: bytes from one k-feature to the next
     bool transposed;
     __device__ __forceinline__ StateAt(const float *states, int64_t index, const LinearWalkArgs &a, int row0, int lane)
     {
-        const int row = row0 + (lane & 31), g = lane >> 5;
+        const int row = row0 + (lane & 15), kg = lane >> 4;
         state = __builtin_amdgcn_make_buffer_rsrc((void *)(states + index * a.dv * a.dk), 0, a.dv * a.dk * 4, 0x00020000);
         transposed = a.transposed != 0;
         pitch = transposed ? 4 * a.dv : 4;
         dk = a.dk;
-        lane_offset = row < a.dv ? row * (transposed ? 4 : 4 * a.dk) + 4 * g * pitch : (int)0x80000000;
+        lane_offset = row < a.dv ? row * (transposed ? 4 : 4 * a.dk) + 4 * kg * pitch : (int)0x80000000;
     }
-    // (dk is a multiple of 16: whether a run exists depends on the pair of runs alone)
-    __device__ __forceinline__ bool exists(int jb, int q4) const { return 32 * jb + 16 * (q4 >> 1) < dk; }
-    __device__ __forceinline__ f32x4 load(int jb, int q4) const
+    // (dk is a multiple of 16: a run exists for all lanes or for none)
+    __device__ __forceinline__ f32x4 load(int j) const
     {
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (!exists(jb, q4)) return x;
-        const int at = lane_offset + (32 * jb + 8 * q4) * pitch;
+        if (16 * j >= dk) return x;
+        const int at = lane_offset + 16 * j * pitch;
         if (!transposed) return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(state, at, 0, 0));
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(state, at + e * pitch, 0, 0));
         return x;
     }
-    __device__ __forceinline__ void store(int jb, int q4, f32x4 x) const
+    __device__ __forceinline__ void store(int j, f32x4 x) const
     {
-        if (!exists(jb, q4)) return;
-        const int at = lane_offset + (32 * jb + 8 * q4) * pitch;
+        if (16 * j >= dk) return;
+        const int at = lane_offset + 16 * j * pitch;
         if (!transposed) {
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), state, at, 0, 0);
         } else {
@@ -172,29 +217,31 @@ __device__ __forceinline__ int chunk_offset(const RowTensor &x, int row, int col
 
 enum Group { kOne, kQueries, kSources };           // n_q = n_src = 1; several queries; several sources of a token
 
-// PIECES: of states and masked products in the readout (float32 tensors: 1). DOT: dot_out is wanted.
-template <class MMA, int DK, int NW, int PIECES, bool DOT, bool SUMMARY, Group GROUP>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DK > 128 ? 1 : 2, DK > 128 ? 1 : 2)))
+// Waves on a SIMD that a kernel's registers are limited for: two workgroups of a CU's LDS, one with 256 k-features.
+constexpr int walk_waves(int dk, int nw) { return nw == 8 && dk <= 128 ? 4 : 2; }
+
+// PIECES: of states and masked products in the readout, VW: of the weighted v (float32 tensors: 1). DOT: dot_out is wanted.
+template <class M, int DK, int NW, int PIECES, int VW, bool DOT, bool SUMMARY, Group GROUP>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(walk_waves(DK, NW), walk_waves(DK, NW))))
 void linear_walk_kernel(LinearWalkArgs a)
 {
-    typedef Shape<MMA, DK, NW> SH;
-    typedef typename MMA::frag frag;
-    typedef typename MMA::elem_t elem_t;
-    constexpr bool BF16 = SH::BF16;
-    constexpr int C = SH::C, TB = SH::TB, NT = SH::NT, NBK = SH::NBK, E = SH::E, PK = SH::PK, PV = SH::PV, HS = MMA::HS, ES = SH::ES;
-    constexpr int RSQ = SH::RSQ, RSK = SH::RSK, RSV = SH::RSV;
-    constexpr int VW = BF16 ? 3 : 1;               // pieces of the weighted v (they end in the float32 state)
+    typedef Shape<M, DK, NW> SH;
+    typedef typename SH::QT QT;
+    typedef typename SH::KT KT;
+    typedef typename SH::VT VT;
+    typedef typename M::frag frag;
+    constexpr bool BF16 = M::BF16;
+    constexpr int C = SH::C, TB = SH::TB, SB = SH::SB, NT = SH::NT, NJ = SH::NJ, KB = SH::KB, E = SH::E, ES = SH::ES, PK = SH::PK,
+                  PV = SH::PV, STEPS = M::STEPS, VEC = M::VEC;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    elem_t *sK = (elem_t *)smem;
-    elem_t *sV = (elem_t *)(smem + SH::k_bytes);
-    float *sHi = (float *)(smem + SH::k_bytes + SH::v_bytes), *sLo = sHi + 64, *sW = sLo + 64;
-    elem_t *sQ = (elem_t *)(sW + 64);
-    frag *sP = (frag *)((unsigned char *)sQ + SH::q_bytes);
+    unsigned char *sK = smem, *sV = smem + SH::k_bytes;
+    float *tables = (float *)(sV + SH::v_bytes);   // [2][5][64]: log2 decay (two floats), weight in the state, zeta of a token; zeta_C
+    unsigned char *sQ = (unsigned char *)tables + SH::tables, *sP = sQ + SH::q_bytes;
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 31, g = lane >> 5;
+    const int n = lane & 15, kg = lane >> 4;
     const int n_pairs = a.B * a.Hkv;
     const int pair = blockIdx.x % n_pairs;
     const int slice = blockIdx.x / n_pairs % a.slices;
@@ -204,49 +251,19 @@ void linear_walk_kernel(LinearWalkArgs a)
     const int chunk_begin = seg * a.seg_chunks;
     const int chunk_end = min(chunk_begin + a.seg_chunks, n_chunks);
     const int steps = GROUP == kQueries ? a.n_q : GROUP == kSources ? a.n_src : 1;
-    const int v0 = slice * 32 * NW;                // first feature of the slice
-    const int64_t state_floats = (int64_t)32 * NW * DK;
-
-    // ---- the state that the segment starts from
-    f32x16 acc[NBK];
-#pragma unroll
-    for (int jb = 0; jb < NBK; ++jb) acc[jb] = zero16();
-    if constexpr (!SUMMARY) {
-        if (a.n_segs > 1) {
-            const float *s = a.seg_states + seg_state_at(a, pair, slice, seg, state_floats) + w * NBK * 1024;
-#pragma unroll
-            for (int jb = 0; jb < NBK; ++jb)
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    const f32x4 x = *(const f32x4 *)(s + (jb * 4 + q4) * 256 + 4 * lane);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[jb][4 * q4 + e] = x[e];
-                }
-        } else if (a.init) {
-            const StateAt S(a.init, (int64_t)(b / a.share) * a.Hkv + h, a, v0 + 32 * w, lane);
-#pragma unroll
-            for (int jb = 0; jb < NBK; ++jb)
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    const f32x4 x = S.load(jb, q4);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[jb][4 * q4 + e] = x[e];
-                }
-        }
-    }
+    const int v0 = slice * 16 * NW;                // first feature of the slice
+    constexpr int64_t state_floats = (int64_t)16 * NW * DK;
 
     // ---- rows of a chunk: memory -> registers (a step ahead) -> LDS
     struct Rows {
         u32x4_t q[SUMMARY ? 1 : PK], k[PK], v[PV];
-        float gate;
     };
-    constexpr int KROW = DK / E, VROW = 32 * NW / E;          // pieces of a row
-    const int krow = tid / KROW, kcol = E * (tid % KROW);     // (a thread's pieces all lie in one column)
-    const int vrow = tid / VROW, vcol = E * (tid % VROW);
-    const bool k_in = kcol < a.dk, v_in = v0 + vcol < a.dv;
-    const int q_off = chunk_offset<ES>(a.q, krow, kcol, k_in, a.reverse);
-    const int k_off = chunk_offset<ES>(a.k, krow, kcol, k_in, a.reverse);
-    const int v_off = chunk_offset<ES>(a.v, vrow, v0 + vcol, v_in, a.reverse);
+    constexpr int KROW = DK / E, VROW = 16 * NW / E;          // pieces of a row
+    const int krow = tid / KROW, kpiece = tid % KROW;         // (a thread's pieces all lie in one column)
+    const int vrow = tid / VROW, vpiece = tid % VROW;
+    const int q_off = chunk_offset<ES>(a.q, krow, E * kpiece, E * kpiece < a.dk, a.reverse);
+    const int k_off = chunk_offset<ES>(a.k, krow, E * kpiece, E * kpiece < a.dk, a.reverse);
+    const int v_off = chunk_offset<ES>(a.v, vrow, v0 + E * vpiece, v0 + E * vpiece < a.dv, a.reverse);
     auto fetch_rows = [&](auto &to, const RowTensor &x, int head, int tau0, int offset, int rows_per) {
         const ChunkRows r = chunk_rows<C, ES>(x, b, head, tau0, a.T, a.reverse);
         const int step = chunk_offset<ES>(x, rows_per, 0, true, a.reverse);
@@ -262,201 +279,202 @@ void linear_walk_kernel(LinearWalkArgs a)
             fetch_rows(f.k, a.k, head, c * C, k_off, NT / KROW);
             fetch_rows(f.v, a.v, head, c * C, v_off, NT / VROW);
         }
-        if (s == 0) {
-            const int tau = c * C + lane;
-            f.gate = 1.0f;
-            if (lane < C && tau < a.T && !(a.reverse && tau == 0))
-                f.gate = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + (a.reverse ? a.T - tau : tau)) * a.Hkv + h];
-        }
     };
     auto stage = [&](const Rows &f, int s) {
         if constexpr (!SUMMARY)
             if (GROUP == kQueries || s == 0) {
 #pragma unroll
-                for (int i = 0; i < PK; ++i) *(u32x4_t *)(sQ + (krow + i * (NT / KROW)) * RSQ + kcol) = f.q[i];
+                for (int i = 0; i < PK; ++i) {
+                    const int row = krow + i * (NT / KROW);
+                    if constexpr (BF16) {
+                        const int j = kpiece & 3, to = kpiece & ~3, half = 8 * (j >> 1);
+                        *(u32x2_t *)(sQ + QT::at(row, to + (2 * j & 3)) + half) = u32x2_t{f.q[i][0], f.q[i][1]};
+                        *(u32x2_t *)(sQ + QT::at(row, to + (2 * j & 3) + 1) + half) = u32x2_t{f.q[i][2], f.q[i][3]};
+                    } else {
+                        *(u32x4_t *)(sQ + QT::at(row, kpiece)) = f.q[i];
+                    }
+                }
             }
         if (GROUP == kSources || s == 0) {
 #pragma unroll
-            for (int i = 0; i < PK; ++i) *(u32x4_t *)(sK + (krow + i * (NT / KROW)) * RSK + kcol) = f.k[i];
+            for (int i = 0; i < PK; ++i) *(u32x4_t *)(sK + KT::at(krow + i * (NT / KROW), kpiece)) = f.k[i];
 #pragma unroll
-            for (int i = 0; i < PV; ++i) *(u32x4_t *)(sV + (vrow + i * (NT / VROW)) * RSV + vcol) = f.v[i];
+            for (int i = 0; i < PV; ++i) *(u32x4_t *)(sV + VT::at(vrow + i * (NT / VROW), vpiece)) = f.v[i];
         }
     };
 
-    float seg_decay = 1.0f;
+    // ---- decays: the last wave leaves those of the next chunk in the tables, lane j those of token j
+    float gate = 1.0f, seg_decay = 1.0f;
+    auto fetch_gate = [&](int c) {
+        const int tau = c * C + lane;
+        gate = 1.0f;
+        if (lane < C && tau < a.T && !(a.reverse && tau == 0))
+            gate = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + (a.reverse ? a.T - tau : tau)) * a.Hkv + h];
+    };
+    auto decays = [&](int c) {
+        const double G = wave_inclusive_scan_f64((double)log2_gate(gate)), total = lane63_f64(G);
+        const float hi = (float)G, zeta_C = __builtin_amdgcn_exp2f((float)total);
+        float *t = tables + (c & 1) * 320 + lane;
+        t[0] = hi;
+        t[64] = (float)(G - (double)hi);
+        t[128] = c * C + lane < a.T ? __builtin_amdgcn_exp2f((float)(total - G)) : 0.0f;
+        t[192] = __builtin_amdgcn_exp2f(hi);
+        t[256] = zeta_C;
+        seg_decay *= zeta_C;
+    };
+
     Rows rows;
     fetch(rows, chunk_begin, 0);
+    if (w == NW - 1) fetch_gate(chunk_begin);
+
+    // ---- the state that the segment starts from
+    f32x4 acc[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (!SUMMARY) {
+        const float *s = a.seg_states + seg_state_at(a, pair, slice, 0, state_floats) + (w * NJ * 64 + lane) * 4;
+        if (a.n_segs > 1 && a.scanned) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[j] = *(const f32x4 *)(s + seg * state_floats + j * 256);
+        } else {
+            if (a.init) {
+                const StateAt S(a.init, (int64_t)(b / a.share) * a.Hkv + h, a, v0 + 16 * w, lane);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[j] = S.load(j);
+            }
+            for (int before = 0; before < seg; ++before) {
+                const float decay = a.seg_decay[(int64_t)pair * a.n_segs + before];
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const f32x4 adds = *(const f32x4 *)(s + before * state_floats + j * 256);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[j][r] = decay * acc[j][r] + adds[r];
+                }
+            }
+        }
+    }
+
+    if (w == NW - 1) decays(chunk_begin);
     for (int c = chunk_begin; c < chunk_end; ++c) {
-        // ---- decays of the chunk (every wave for itself): lane j holds token j
-        const double G = wave_inclusive_scan_f64((double)log2_gate(rows.gate));
-        const double Gtot = lane63_f64(G);
-        const float g_hi = (float)G, g_lo = (float)(G - (double)g_hi);
-        const float zeta_C = __builtin_amdgcn_exp2f((float)Gtot);
-        const float w_j = c * C + lane < a.T ? __builtin_amdgcn_exp2f((float)(Gtot - G)) : 0.0f;   // of token j in the state after the chunk
-        seg_decay *= zeta_C;
-        f32x16 y[TB];
+        const float *sHi = tables + (c & 1) * 320, *sLo = sHi + 64, *sW = sHi + 128, *sZ = sHi + 192;
+        f32x4 y[TB];
         for (int s = 0; s < steps; ++s) {
             lds_barrier();                         // the tiles of the step before have been read
             stage(rows, s);
-            if (s == 0 && w == 0) {
-                sHi[lane] = g_hi;
-                sLo[lane] = g_lo;
-                sW[lane] = w_j;
-            }
-            __builtin_amdgcn_sched_barrier(0);
             if (s + 1 < steps) fetch(rows, c, s + 1);
             else if (c + 1 < chunk_end) fetch(rows, c + 1, 0);
+            if (w == NW - 1 && s + 1 == steps && c + 1 < chunk_end) fetch_gate(c + 1);
             lds_barrier();                         // (no wait for the rows in flight)
             __builtin_amdgcn_sched_barrier(0);
 
             if constexpr (!SUMMARY) {
-                // ---- products K Q^T of the causal tiles (key block sb, token block tb)
-                // M[t, s] on register r of lane (n, g): token 32 tb + n, key 32 sb + kidx(r, g)
-                auto masked = [&](const f32x16 &x, int sb, int tb, float (&m)[16]) {
-                    const float hi = sHi[32 * tb + n], lo = sLo[32 * tb + n];
-                    const int t = 32 * (tb - sb) + n;          // (in the tile below the diagonal: above every key)
+                // ---- masked products M[t, s] (k_s . q_t): a unit is a block of 16 tokens and 32 keys, left as operand fragments
+                for (int unit = w; unit < SH::UNITS; unit += NW) {
+                    const int tb = unit < 2 ? unit : 1 + unit / 2, sb = unit < 2 ? 0 : unit & 1;
+                    f32x4 x[2];
 #pragma unroll
-                    for (int q4 = 0; q4 < 4; ++q4) {
-                        const int s0 = 32 * sb + 8 * q4 + 4 * g;
+                    for (int half = 0; half < 2; ++half) {
+                        x[half] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        if (2 * sb + half > tb) continue;
+#pragma unroll
+                        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                            for (int st = 0; st < STEPS; ++st)
+                                x[half] = M::mma(k_row_frag<M, KT>(sK, 32 * sb + 16 * half + n, kb, st, kg),
+                                                 q_frag<M, QT>(sQ, 16 * tb + n, kb, st, kg), x[half]);
+                    }
+                    // register r: key 32 sb + 16 half + 4 kg + r, token 16 tb + n
+                    const float hi = sHi[16 * tb + n], lo = sLo[16 * tb + n];
+                    float m[8];
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const int s0 = 32 * sb + 16 * half + 4 * kg;
                         const f32x4 h4 = *(const f32x4 *)(sHi + s0), l4 = *(const f32x4 *)(sLo + s0);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            m[4 * q4 + e] = 8 * q4 + 4 * g + e <= t
-                                                ? x[4 * q4 + e] * __builtin_amdgcn_exp2f((hi - h4[e]) + (lo - l4[e]))
-                                                : 0.0f;
-                    }
-                };
-                if constexpr (BF16) {
-                    // a tile to a wave; masked, cut into pieces and left as operand fragments
-                    for (int tile = w; tile < 3; tile += NW) {
-                        const int sb = tile >> 1, tb = (tile + 1) >> 1;
-                        f32x16 x = zero16();
-                        const elem_t *krow_p = sK + (32 * sb + n) * RSK, *qrow_p = sQ + (32 * tb + n) * RSQ;
-#pragma unroll
-                        for (int st = 0; st < NBK * HS; ++st)
-                            x = MMA::mma(row_frag(krow_p, st / HS, st % HS, g), row_frag(qrow_p, st / HS, st % HS, g), x);
-                        float m[16];
-                        masked(x, sb, tb, m);
-#pragma unroll
-                        for (int st = 0; st < HS; ++st) {
-                            frag f[PIECES];
-                            cut<MMA, PIECES>(m + MMA::VEC * st, f);
-#pragma unroll
-                            for (int i = 0; i < PIECES; ++i) sP[((i * 3 + tile) * HS + st) * 64 + lane] = f[i];
-                        }
-                    }
-                } else {
-                    // the one tile: every wave adds the products of its share of the features
-                    f32x16 x = zero16();
-#pragma unroll
-                    for (int j = 0; j < (NBK + NW - 1) / NW; ++j) {
-                        const int jb = j * NW + w;
-                        if (jb < NBK)
-#pragma unroll
-                            for (int st = 0; st < HS; ++st)
-                                x = MMA::mma(row_frag(sK + n * RSK, jb, st, g), row_frag(sQ + n * RSQ, jb, st, g), x);
+                        for (int r = 0; r < 4; ++r)
+                            m[4 * half + r] = s0 + r <= 16 * tb + n ? x[half][r] * __builtin_amdgcn_exp2f((hi - h4[r]) + (lo - l4[r])) : 0.0f;
                     }
 #pragma unroll
-                    for (int q4 = 0; q4 < 4; ++q4)
-                        *(f32x4 *)((float *)sP + w * 1024 + q4 * 256 + 4 * lane) = f32x4{x[4 * q4], x[4 * q4 + 1], x[4 * q4 + 2], x[4 * q4 + 3]};
+                    for (int st = 0; st < STEPS; ++st) {
+                        frag f[PIECES];
+                        cut<M, PIECES>(m + VEC * st, f);
+#pragma unroll
+                        for (int i = 0; i < PIECES; ++i) ((frag *)sP)[((i * SH::UNITS + unit) * STEPS + st) * 64 + lane] = f[i];
+                    }
                 }
                 __builtin_amdgcn_sched_barrier(0);
 
-                // ---- zeta_t S_[n] q_t: the state's tiles are the A operand
+                // ---- zeta_t S_[n] q_t: pairs of the state's tiles are the A operand
                 if (GROUP == kQueries || s == 0) {
 #pragma unroll
-                    for (int tb = 0; tb < TB; ++tb) y[tb] = zero16();
+                    for (int tb = 0; tb < TB; ++tb) y[tb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int jb = 0; jb < NBK; ++jb)
+                    for (int kb = 0; kb < KB; ++kb) {
+                        const float x[8] = {acc[2 * kb][0], acc[2 * kb][1], acc[2 * kb][2], acc[2 * kb][3],
+                                            acc[2 * kb + 1][0], acc[2 * kb + 1][1], acc[2 * kb + 1][2], acc[2 * kb + 1][3]};
 #pragma unroll
-                        for (int st = 0; st < HS; ++st) {
-                            float x[MMA::VEC];
-#pragma unroll
-                            for (int e = 0; e < MMA::VEC; ++e) x[e] = acc[jb][MMA::VEC * st + e];
+                        for (int st = 0; st < STEPS; ++st) {
                             frag f[PIECES];
-                            cut<MMA, PIECES>(x, f);
+                            cut<M, PIECES>(x + VEC * st, f);
 #pragma unroll
                             for (int tb = 0; tb < TB; ++tb) {
-                                const frag qf = row_frag(sQ + (32 * tb + n) * RSQ, jb, st, g);
+                                const frag qf = q_frag<M, QT>(sQ, 16 * tb + n, kb, st, kg);
 #pragma unroll
-                                for (int i = 0; i < PIECES; ++i) y[tb] = MMA::mma(f[i], qf, y[tb]);
+                                for (int i = 0; i < PIECES; ++i) y[tb] = M::mma(f[i], qf, y[tb]);
                             }
                         }
+                    }
 #pragma unroll
                     for (int tb = 0; tb < TB; ++tb) {
-                        const float zeta = __builtin_amdgcn_exp2f(sHi[32 * tb + n]);
+                        const float zeta = sZ[16 * tb + n];
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) y[tb][r] *= zeta;
+                        for (int r = 0; r < 4; ++r) y[tb][r] *= zeta;
                     }
                 }
                 lds_barrier();                     // the masked products are there
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if (w == NW - 1 && s + 1 == steps && c + 1 < chunk_end) decays(c + 1);
 
-            frag vt[TB][HS];                       // v, features on the lanes, tokens in kidx order
+            frag vt[SB][STEPS];                    // v, features on the lanes, contraction over the tokens
 #pragma unroll
-            for (int sb = 0; sb < TB; ++sb)
+            for (int sb = 0; sb < SB; ++sb)
 #pragma unroll
-                for (int st = 0; st < HS; ++st) vt[sb][st] = col_frag(sV, RSV, 32 * w, sb, st, lane);
+                for (int st = 0; st < STEPS; ++st) vt[sb][st] = col_frag<M, VT>(sV, w, sb, st, lane);
 
             if constexpr (!SUMMARY) {
                 // ---- + sum_s v_s M[t, s] (k_s . q_t)
-                if constexpr (BF16) {
 #pragma unroll
-                    for (int tile = 0; tile < 3; ++tile) {
-                        const int sb = tile == 2 ? 1 : 0, tb = tile == 0 ? 0 : 1;
+                for (int unit = 0; unit < SH::UNITS; ++unit) {
+                    const int tb = unit < 2 ? unit : 1 + unit / 2, sb = unit < 2 ? 0 : unit & 1;
 #pragma unroll
-                        for (int st = 0; st < HS; ++st)
+                    for (int st = 0; st < STEPS; ++st)
 #pragma unroll
-                            for (int i = 0; i < PIECES; ++i)
-                                y[tb] = MMA::mma(vt[sb][st], sP[((i * 3 + tile) * HS + st) * 64 + lane], y[tb]);
-                    }
-                } else {
-                    f32x16 x = zero16();
-#pragma unroll
-                    for (int i = 0; i < NW; ++i)
-#pragma unroll
-                        for (int q4 = 0; q4 < 4; ++q4) {
-                            const f32x4 part = *(const f32x4 *)((const float *)sP + i * 1024 + q4 * 256 + 4 * lane);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) x[4 * q4 + e] += part[e];
-                        }
-                    const float hi = sHi[n], lo = sLo[n];
-                    float m[16];
-#pragma unroll
-                    for (int q4 = 0; q4 < 4; ++q4) {
-                        const f32x4 h4 = *(const f32x4 *)(sHi + 8 * q4 + 4 * g), l4 = *(const f32x4 *)(sLo + 8 * q4 + 4 * g);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            m[4 * q4 + e] = 8 * q4 + 4 * g + e <= n ? x[4 * q4 + e] * __builtin_amdgcn_exp2f((hi - h4[e]) + (lo - l4[e])) : 0.0f;
-                    }
-#pragma unroll
-                    for (int st = 0; st < HS; ++st) y[0] = MMA::mma(vt[0][st], m[st], y[0]);
+                        for (int i = 0; i < PIECES; ++i)
+                            y[tb] = M::mma(vt[sb][st], ((const frag *)sP)[((i * SH::UNITS + unit) * STEPS + st) * 64 + lane], y[tb]);
                 }
-                // ---- out: lane (n, g) holds features v0 + 32 w + kidx(r, g) of token 32 tb + n
+                // ---- out: register r holds feature v0 + 16 w + 4 kg + r of token 16 tb + n
                 if (GROUP == kQueries || s + 1 == steps) {
                     const int head = GROUP == kQueries ? h * steps + s : h;
+                    const int col = v0 + 16 * w + 4 * kg;
+                    const bool in = v0 + 16 * w < a.dv;
                     if constexpr (DOT) {
                         float *sDot = (float *)sP; // [NW][C], in place of the masked products
                         const ChunkRows r = chunk_rows<C, ES>(a.dot_with, b, head, c * C, a.T, a.reverse);
                         lds_barrier();
 #pragma unroll
                         for (int tb = 0; tb < TB; ++tb) {
+                            const int at = chunk_offset<ES>(a.dot_with, 16 * tb + n, col, in, a.reverse) + r.top;
+                            f32x4 x;
+                            if constexpr (BF16)
+                                x = IOBF16::cvt4(__builtin_bit_cast(u16x4, __builtin_amdgcn_raw_buffer_load_b64(r.rows, at, 0, 0)));
+                            else
+                                x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r.rows, at, 0, 0));
                             float dot = 0.0f;
 #pragma unroll
-                            for (int q4 = 0; q4 < 4; ++q4) {
-                                const int col = v0 + 32 * w + 8 * q4 + 4 * g;
-                                const int at = chunk_offset<ES>(a.dot_with, 32 * tb + n, col, col < a.dv, a.reverse) + r.top;
-                                f32x4 x;
-                                if constexpr (BF16)
-                                    x = IOBF16::cvt4(__builtin_bit_cast(u16x4, __builtin_amdgcn_raw_buffer_load_b64(r.rows, at, 0, 0)));
-                                else
-                                    x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r.rows, at, 0, 0));
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) dot += x[e] * y[tb][4 * q4 + e];
-                            }
-                            dot += __shfl_xor(dot, 32, 64);
-                            if (g == 0) sDot[w * C + 32 * tb + n] = dot;
+                            for (int e = 0; e < 4; ++e) dot += x[e] * y[tb][e];
+                            dot = sum_over_kg(dot);
+                            if (kg == 0) sDot[w * C + 16 * tb + n] = dot;
                         }
                         lds_barrier();
                         if (w == 0 && lane < C && c * C + lane < a.T) {
@@ -468,34 +486,28 @@ void linear_walk_kernel(LinearWalkArgs a)
                         }
                     }
                     const ChunkRows out = chunk_rows<C, ES>(a.y, b, head, c * C, a.T, a.reverse);
+                    if constexpr (BF16) {
+                        // (lanes of neighbouring kg exchange runs of two token blocks, so that a lane stores eight features at once)
 #pragma unroll
-                    for (int tb = 0; tb < TB; ++tb) {
-                        if constexpr (BF16) {
-                            // (the halves of the wave exchange runs, so that a lane stores eight features at once)
-                            u32x2_t x[4];
+                        for (int tb = 0; tb < TB; tb += 2) {
+                            u32x2_t x[2];
 #pragma unroll
-                            for (int q4 = 0; q4 < 4; ++q4) {
-                                const u16x4 o = {f32_to_bf16_bits(y[tb][4 * q4]), f32_to_bf16_bits(y[tb][4 * q4 + 1]),
-                                                 f32_to_bf16_bits(y[tb][4 * q4 + 2]), f32_to_bf16_bits(y[tb][4 * q4 + 3])};
-                                x[q4] = __builtin_bit_cast(u32x2_t, o);
+                            for (int i = 0; i < 2; ++i) {
+                                const u16x4 o = {f32_to_bf16_bits(y[tb + i][0]), f32_to_bf16_bits(y[tb + i][1]), f32_to_bf16_bits(y[tb + i][2]),
+                                                 f32_to_bf16_bits(y[tb + i][3])};
+                                x[i] = __builtin_bit_cast(u32x2_t, o);
                             }
-#pragma unroll
-                            for (int p = 0; p < 2; ++p) {
-                                const auto r0 = __builtin_amdgcn_permlane32_swap(x[2 * p][0], x[2 * p + 1][0], false, false);
-                                const auto r1 = __builtin_amdgcn_permlane32_swap(x[2 * p][1], x[2 * p + 1][1], false, false);
-                                const int col = v0 + 32 * w + 16 * p + 8 * g;
-                                __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{r0[0], r1[0], r0[1], r1[1]}, out.rows,
-                                                                       chunk_offset<ES>(a.y, 32 * tb + n, col, col < a.dv, a.reverse) + out.top, 0, 0);
-                            }
-                        } else {
-#pragma unroll
-                            for (int q4 = 0; q4 < 4; ++q4) {
-                                const int col = v0 + 32 * w + 8 * q4 + 4 * g;
-                                const f32x4 x = {y[tb][4 * q4], y[tb][4 * q4 + 1], y[tb][4 * q4 + 2], y[tb][4 * q4 + 3]};
-                                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), out.rows,
-                                                                       chunk_offset<ES>(a.y, 32 * tb + n, col, col < a.dv, a.reverse) + out.top, 0, 0);
-                            }
+                            const auto r0 = __builtin_amdgcn_permlane16_swap(x[0][0], x[1][0], false, false);
+                            const auto r1 = __builtin_amdgcn_permlane16_swap(x[0][1], x[1][1], false, false);
+                            // even kg: features 4 kg .. + 7 of block tb; odd kg: 4 (kg - 1) .. + 7 of block tb + 1
+                            const int at = chunk_offset<ES>(a.y, 16 * (tb + (kg & 1)) + n, v0 + 16 * w + 4 * (kg & 2), in, a.reverse) + out.top;
+                            __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{r0[0], r1[0], r0[1], r1[1]}, out.rows, at, 0, 0);
                         }
+                    } else {
+#pragma unroll
+                        for (int tb = 0; tb < TB; ++tb)
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, y[tb]), out.rows,
+                                                                   chunk_offset<ES>(a.y, 16 * tb + n, col, in, a.reverse) + out.top, 0, 0);
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -503,83 +515,67 @@ void linear_walk_kernel(LinearWalkArgs a)
 
             // ---- S <- zeta_C S + sum_s w_s v_s k_s^T
             if (GROUP == kSources ? s == 0 : s + 1 == steps) {
+                const float zeta_C = sHi[256];
 #pragma unroll
-                for (int jb = 0; jb < NBK; ++jb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[jb][r] *= zeta_C;
+                for (int j = 0; j < NJ; ++j) acc[j] *= zeta_C;
             }
             if (GROUP == kSources || s + 1 == steps) {
 #pragma unroll
-                for (int sb = 0; sb < TB; ++sb)
+                for (int sb = 0; sb < SB; ++sb) {
+                    const f32x4 w0 = *(const f32x4 *)(sW + 32 * sb + 4 * kg), w1 = *(const f32x4 *)(sW + 32 * sb + 16 + 4 * kg);
+                    const float wt[8] = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
 #pragma unroll
-                    for (int st = 0; st < HS; ++st) {
-                        float x[MMA::VEC];
-                        MMA::unpack(vt[sb][st], x);
-                        if constexpr (BF16) {
-                            const int t0 = 32 * sb + 16 * st + 4 * g;
-                            const f32x4 w0 = *(const f32x4 *)(sW + t0), w1 = *(const f32x4 *)(sW + t0 + 8);
+                    for (int st = 0; st < STEPS; ++st) {
+                        float x[VEC];
+                        M::unpack(vt[sb][st], x);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                x[e] *= w0[e];
-                                x[4 + e] *= w1[e];
-                            }
-                        } else {
-                            x[0] *= sW[kidx(st, g)];
-                        }
+                        for (int e = 0; e < VEC; ++e) x[e] *= wt[VEC * st + e];
                         frag f[VW];
-                        cut<MMA, VW>(x, f);
+                        cut<M, VW>(x, f);
 #pragma unroll
-                        for (int jb = 0; jb < NBK; ++jb) {
-                            const frag kt = col_frag(sK, RSK, 32 * jb, sb, st, lane);
+                        for (int j = 0; j < NJ; ++j) {
+                            const frag kt = col_frag<M, KT>(sK, j, sb, st, lane);
 #pragma unroll
-                            for (int i = 0; i < VW; ++i) acc[jb] = MMA::mma(kt, f[i], acc[jb]);
+                            for (int i = 0; i < VW; ++i) acc[j] = M::mma(kt, f[i], acc[j]);
                         }
                     }
+                }
             }
         }
     }
 
     if constexpr (SUMMARY) {
-        float *s = a.seg_states + seg_state_at(a, pair, slice, seg, state_floats) + w * NBK * 1024;
+        float *s = a.seg_states + seg_state_at(a, pair, slice, seg, state_floats) + (w * NJ * 64 + lane) * 4;
 #pragma unroll
-        for (int jb = 0; jb < NBK; ++jb)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4)
-                *(f32x4 *)(s + (jb * 4 + q4) * 256 + 4 * lane) =
-                    f32x4{acc[jb][4 * q4], acc[jb][4 * q4 + 1], acc[jb][4 * q4 + 2], acc[jb][4 * q4 + 3]};
-        if (tid == 0 && slice == 0) a.seg_decay[(int64_t)pair * a.n_segs + seg] = seg_decay;
+        for (int j = 0; j < NJ; ++j) *(f32x4 *)(s + j * 256) = acc[j];
+        if (w == NW - 1 && lane == 0 && slice == 0) a.seg_decay[(int64_t)pair * a.n_segs + seg] = seg_decay;
     } else if (seg == a.n_segs - 1) {
         if (a.state_dot_out) {
-            const StateAt S(a.state_dot_with, pair, a, v0 + 32 * w, lane);
+            const StateAt S(a.state_dot_with, pair, a, v0 + 16 * w, lane);
             float dot = 0.0f;
 #pragma unroll
-            for (int jb = 0; jb < NBK; ++jb)
+            for (int j = 0; j < NJ; ++j) {
+                const f32x4 x = S.load(j);
 #pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    const f32x4 x = S.load(jb, q4);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) dot += x[e] * acc[jb][4 * q4 + e];
-                }
+                for (int e = 0; e < 4; ++e) dot += x[e] * acc[j][e];
+            }
             dot = wave_sum(dot);
             lds_barrier();
-            if (lane == 0) sHi[w] = dot;
+            if (lane == 0) tables[w] = dot;
             lds_barrier();
             if (tid == 0) {
                 float all = 0.0f;
 #pragma unroll
-                for (int i = 0; i < NW; ++i) all += sHi[i];
+                for (int i = 0; i < NW; ++i) all += tables[i];
                 a.state_dot_out[(int64_t)slice * n_pairs + pair] = all;
             }
         }
         if (a.final) {
-            const StateAt S(a.final, pair, a, v0 + 32 * w, lane);
+            const StateAt S(a.final, pair, a, v0 + 16 * w, lane);
             float scale = 1.0f;
             if (a.final_times_gate) scale = __builtin_amdgcn_exp2f(log2_gate(a.gate_per_head ? a.gate[h] : a.gate[(int64_t)b * a.T * a.Hkv + h]));
 #pragma unroll
-            for (int jb = 0; jb < NBK; ++jb)
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4)
-                    S.store(jb, q4, f32x4{acc[jb][4 * q4], acc[jb][4 * q4 + 1], acc[jb][4 * q4 + 2], acc[jb][4 * q4 + 3]} * scale);
+            for (int j = 0; j < NJ; ++j) S.store(j, acc[j] * scale);
         }
     }
 }
@@ -588,21 +584,17 @@ void linear_walk_kernel(LinearWalkArgs a)
 template <int DK, int NW>
 __global__ __launch_bounds__(256) void linear_scan_kernel(LinearWalkArgs a)
 {
-    constexpr int NBK = DK / 32;
-    constexpr int64_t state_floats = (int64_t)32 * NW * DK;
+    constexpr int NJ = DK / 16;
+    constexpr int64_t state_floats = (int64_t)16 * NW * DK;
     constexpr int BLOCKS = (int)(state_floats / 1024);         // workgroups for a state of a slice
     const int part = blockIdx.x % BLOCKS;
     const int slice = blockIdx.x / BLOCKS % a.slices;
     const int pair = blockIdx.x / BLOCKS / a.slices;
     const int b = pair / a.Hkv, h = pair % a.Hkv;
-    const int at = (part * 256 + threadIdx.x) * 4;             // ((w NBK + jb) 4 + q4) 256 + 4 lane
-    float *s = a.seg_states + seg_state_at(a, pair, slice, 0, state_floats) + at;
+    const int tile = __builtin_amdgcn_readfirstlane(part * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;   // tile: w NJ + j
+    float *s = a.seg_states + seg_state_at(a, pair, slice, 0, state_floats) + (tile * 64 + lane) * 4;
     f32x4 run = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (a.init) {
-        const int lane = at / 4 % 64, q4 = at / 256 % 4, jb = at / 1024 % NBK, w = at / 1024 / NBK;
-        const StateAt S(a.init, (int64_t)(b / a.share) * a.Hkv + h, a, slice * 32 * NW + 32 * __builtin_amdgcn_readfirstlane(w), lane);
-        run = S.load(__builtin_amdgcn_readfirstlane(jb), __builtin_amdgcn_readfirstlane(q4));
-    }
+    if (a.init) run = StateAt(a.init, (int64_t)(b / a.share) * a.Hkv + h, a, slice * 16 * NW + 16 * (tile / NJ), lane).load(tile % NJ);
     const float *decay = a.seg_decay + (int64_t)pair * a.n_segs;
     f32x4 next = *(const f32x4 *)s;
     for (int seg = 0; seg < a.n_segs; ++seg) {
@@ -613,40 +605,51 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(LinearWalkArgs a)
     }
 }
 
-template <class MMA, int DK, int NW, int PIECES, bool DOT, bool SUMMARY, Group GROUP>
+template <class M, int DK, int NW, int PIECES, int VW, bool DOT, bool SUMMARY, Group GROUP>
 hipError_t launch_kernel(const LinearWalkArgs &a, int workgroups, hipStream_t stream)
 {
-    typedef Shape<MMA, DK, NW> SH;
+    typedef Shape<M, DK, NW> SH;
     constexpr size_t lds = SH::lds_bytes(PIECES, SUMMARY);
+    static_assert(lds <= (size_t)160 << 10, "LDS of a CU");
     static bool raised[kMaxLdsDevices] = {};
-    const hipError_t e = raise_lds_limits(raised, {{(const void *)linear_walk_kernel<MMA, DK, NW, PIECES, DOT, SUMMARY, GROUP>, lds}});
+    const hipError_t e = raise_lds_limits(raised, {{(const void *)linear_walk_kernel<M, DK, NW, PIECES, VW, DOT, SUMMARY, GROUP>, lds}});
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((linear_walk_kernel<MMA, DK, NW, PIECES, DOT, SUMMARY, GROUP>), dim3(workgroups), dim3(SH::NT), lds, stream, a);
+    hipLaunchKernelGGL((linear_walk_kernel<M, DK, NW, PIECES, VW, DOT, SUMMARY, GROUP>), dim3(workgroups), dim3(SH::NT), lds, stream, a);
     return hipGetLastError();
 }
 
-template <class MMA, int DK, int NW, Group GROUP>
-hipError_t launch_walk(const LinearWalkArgs &a, hipStream_t stream)
+// VW: pieces of the weighted v
+template <class M, int DK, int NW, Group GROUP, int VW>
+hipError_t launch_walk_vw(const LinearWalkArgs &a, hipStream_t stream)
 {
-    constexpr bool BF16 = Shape<MMA, DK, NW>::BF16;
     const int n = a.B * a.Hkv * a.slices;
     if (a.n_segs > 1) {
-        hipError_t e = launch_kernel<MMA, DK, NW, 1, false, true, GROUP == kSources ? kSources : kOne>(a, n * (a.n_segs - 1), stream);
+        hipError_t e = launch_kernel<M, DK, NW, 1, VW, false, true, GROUP == kSources ? kSources : kOne>(a, n * (a.n_segs - 1), stream);
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((linear_scan_kernel<DK, NW>), dim3(n * (32 * NW * DK / 1024)), dim3(256), 0, stream, a);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        if (a.scanned) {
+            hipLaunchKernelGGL((linear_scan_kernel<DK, NW>), dim3(n * (16 * NW * DK / 1024)), dim3(256), 0, stream, a);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
     }
-    return a.dot_out ? launch_kernel<MMA, DK, NW, BF16 ? 3 : 1, true, false, GROUP>(a, n * a.n_segs, stream)
-                     : launch_kernel<MMA, DK, NW, BF16 ? 2 : 1, false, false, GROUP>(a, n * a.n_segs, stream);
+    if constexpr (VW != 2)
+        if (a.dot_out) return launch_kernel<M, DK, NW, M::BF16 ? 3 : 1, VW, true, false, GROUP>(a, n * a.n_segs, stream);
+    return launch_kernel<M, DK, NW, M::BF16 ? 2 : 1, VW, false, false, GROUP>(a, n * a.n_segs, stream);
 }
 
-template <class MMA, int DK>
+template <class M, int DK, int NW, Group GROUP>
+hipError_t launch_walk(const LinearWalkArgs &a, hipStream_t stream)
+{
+    if constexpr (M::BF16) return a.dot_out || a.final ? launch_walk_vw<M, DK, NW, GROUP, 3>(a, stream) : launch_walk_vw<M, DK, NW, GROUP, 2>(a, stream);
+    else return launch_walk_vw<M, DK, NW, GROUP, 1>(a, stream);
+}
+
+template <class M, int DK>
 hipError_t launch_walk_dk(const LinearWalkArgs &a, hipStream_t stream)
 {
     const bool narrow = a.dv <= 64;
-    if (a.n_q > 1) return narrow ? launch_walk<MMA, DK, 2, kQueries>(a, stream) : launch_walk<MMA, DK, 4, kQueries>(a, stream);
-    if (a.n_src > 1) return narrow ? launch_walk<MMA, DK, 2, kSources>(a, stream) : launch_walk<MMA, DK, 4, kSources>(a, stream);
-    return narrow ? launch_walk<MMA, DK, 2, kOne>(a, stream) : launch_walk<MMA, DK, 4, kOne>(a, stream);
+    if (a.n_q > 1) return narrow ? launch_walk<M, DK, 4, kQueries>(a, stream) : launch_walk<M, DK, 8, kQueries>(a, stream);
+    if (a.n_src > 1) return narrow ? launch_walk<M, DK, 4, kSources>(a, stream) : launch_walk<M, DK, 8, kSources>(a, stream);
+    return narrow ? launch_walk<M, DK, 4, kOne>(a, stream) : launch_walk<M, DK, 8, kOne>(a, stream);
 }
 
 }  // namespace linear
