@@ -342,11 +342,19 @@ void linear_walk_kernel(LinearWalkArgs a)
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) acc[j] = S.load(j);
             }
+            // (the next segment's in flight while one is added)
+            f32x4 next[NJ];
+            if (seg > 0) {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) next[j] = *(const f32x4 *)(s + j * 256);
+            }
             for (int before = 0; before < seg; ++before) {
                 const float decay = a.seg_decay[(int64_t)pair * a.n_segs + before];
+                const int64_t behind = (before + 1 < seg ? before + 1 : before) * state_floats;
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
-                    const f32x4 adds = *(const f32x4 *)(s + before * state_floats + j * 256);
+                    const f32x4 adds = next[j];
+                    next[j] = *(const f32x4 *)(s + behind + j * 256);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[j][r] = decay * acc[j][r] + adds[r];
                 }
@@ -354,7 +362,10 @@ void linear_walk_kernel(LinearWalkArgs a)
         }
     }
 
-    if (w == NW - 1) decays(chunk_begin);
+    if (w == NW - 1) {
+        decays(chunk_begin);
+        fetch_gate(chunk_begin + 1);
+    }
     for (int c = chunk_begin; c < chunk_end; ++c) {
         const float *sHi = tables + (c & 1) * 320, *sLo = sHi + 64, *sW = sHi + 128, *sZ = sHi + 192;
         f32x4 y[TB];
@@ -363,9 +374,12 @@ void linear_walk_kernel(LinearWalkArgs a)
             stage(rows, s);
             if (s + 1 < steps) fetch(rows, c, s + 1);
             else if (c + 1 < chunk_end) fetch(rows, c + 1, 0);
-            if (w == NW - 1 && s + 1 == steps && c + 1 < chunk_end) fetch_gate(c + 1);
             lds_barrier();                         // (no wait for the rows in flight)
             __builtin_amdgcn_sched_barrier(0);
+            if (w == NW - 1 && s == 0 && c + 1 < chunk_end) {
+                decays(c + 1);                     // (its gates were asked for a chunk ago)
+                fetch_gate(c + 2);
+            }
 
             if constexpr (!SUMMARY) {
                 // ---- masked products M[t, s] (k_s . q_t): a unit is a block of 16 tokens and 32 keys, left as operand fragments
@@ -434,7 +448,6 @@ void linear_walk_kernel(LinearWalkArgs a)
                 lds_barrier();                     // the masked products are there
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (w == NW - 1 && s + 1 == steps && c + 1 < chunk_end) decays(c + 1);
 
             frag vt[SB][STEPS];                    // v, features on the lanes, contraction over the tokens
 #pragma unroll
