@@ -48,55 +48,95 @@ struct Tile16F32 {
     static __device__ __forceinline__ void unpack(frag f, float *x) { x[0] = f; }
 };
 
-// Row-major LDS tile, D elements a row and padding such that the lanes of a read fall into different banks: 16 bytes for reads
-// of 16 rows at one 16-byte piece (and, float32, of 16 columns of 4 rows that are 4 apart), 32 for bf16 transpose reads, 32
-// bytes of 8 rows. Everything but a lane's own base is an offset known when compiling.
+// Row-major LDS tiles, D elements a row. Padded: the lanes of a read fall into different banks for bf16 transpose reads, 32 bytes of
+// 8 rows (32 bytes of padding), and float32 reads of 16 columns of 4 rows that are 4 apart (16). Everything but a lane's own
+// base is then an offset known when compiling.
 template <int D, int ES, int PAD>
-struct Tile {
+struct PaddedTile16 {
     static constexpr int ROW = D * ES + PAD;
     // byte offset of 16-byte piece `piece` of row `row`
     static __device__ __forceinline__ int at(int row, int piece) { return row * ROW + piece * 16; }
+    // `pieces` further in the same row
+    static __device__ __forceinline__ int further(int offset, int pieces) { return offset + pieces * 16; }
+};
+// Swizzled (bf16): no padding, a row's pieces permuted by a XOR. A 16-byte read of 16 rows and two neighbouring pieces runs in groups
+// of 16 lanes, rows 0-3 and 12-15 of one piece with rows 4-11 of the other; a transpose read in halves of 8 rows by 32 bytes. Rows
+// 0-7 are given different pairs of pieces and rows 8-15 the other members of the pairs, in such an order that both reads meet
+// every bank once. (Padded rows instead, d = 128: 24 and 8 cycles for the reads of k rows and q rows, 8 and 4 without conflicts.)
+template <int D>
+struct SwizzledTile16 {
+    static constexpr int PIECES = D / 8, ROW = 2 * D;
+    static __device__ __forceinline__ int swizzle(int row)
+    {
+        if constexpr (PIECES >= 16) return ((row & 7) ^ (row >> 1 & 4)) << 1 | (row >> 3 & 1);
+        else return ((row >> 1 & 3) ^ (row >> 2 & 2)) << 1 | (row >> 3 & 1);
+    }
+    static __device__ __forceinline__ int at(int row, int piece) { return row * ROW + (piece ^ swizzle(row)) * 16; }
+    // (where `pieces` has no bits in common with the piece of `offset`)
+    static __device__ __forceinline__ int further(int offset, int pieces) { return offset ^ pieces * 16; }
 };
 
-// Fragments of step `st` of the contraction over a 32-block `blk`. Rows of q: its LDS tile holds the features of each 32 in the
-// order of the operands (bf16: piece kg of the block is features 4 kg .. + 3 and 16 + 4 kg .. + 3) ...
-template <class M, class T>
-__device__ __forceinline__ typename M::frag q_frag(const unsigned char *tile, int row, int blk, int st, int kg)
+// The value again, as one that the compiler does not know: what is computed from it inside a loop is not kept in registers across
+// it (some thirty offsets into the swizzled tiles, one XOR each, spilled otherwise).
+__device__ __forceinline__ int anew(int x)
 {
-    if constexpr (M::BF16) return __builtin_bit_cast(bf16x8, *(const u32x4_t *)(tile + T::at(row, 4 * blk + kg)));
-    else return (*(const f32x4 *)(tile + T::at(row, 8 * blk + 4 * (st >> 2) + kg)))[st & 3];
+    asm volatile("" : "+v"(x));
+    return x;
 }
-// ... rows of k: theirs lie in natural order, for the transpose reads ...
+
+// Fragments of step `st` of the contraction over a 32-block `blk`, from the lane's own place in the tile (the functions *_place).
+// Rows row0 + n of q: its LDS tile holds the features of each 32 in the order of the operands (bf16: piece kg of the block is
+// features 4 kg .. + 3 and 16 + 4 kg .. + 3) ...
+template <class T>
+__device__ __forceinline__ int q_place(int lane) { return T::at(lane & 15, lane >> 4); }
 template <class M, class T>
-__device__ __forceinline__ typename M::frag k_row_frag(const unsigned char *tile, int row, int blk, int st, int kg)
+__device__ __forceinline__ typename M::frag q_frag(const unsigned char *tile, int place, int row0, int blk, int st)
+{
+    if constexpr (M::BF16) return __builtin_bit_cast(bf16x8, *(const u32x4_t *)(tile + T::further(place, 4 * blk) + row0 * T::ROW));
+    else return (*(const f32x4 *)(tile + T::further(place, 8 * blk + 4 * (st >> 2)) + row0 * T::ROW))[st & 3];
+}
+// ... rows row0 + n of k: theirs lie in natural order, for the transpose reads ...
+template <class M, class T>
+__device__ __forceinline__ int k_place(int lane)
+{
+    if constexpr (M::BF16) return T::at(lane & 15, lane >> 5) + 8 * (lane >> 4 & 1);
+    else return q_place<T>(lane);
+}
+template <class M, class T>
+__device__ __forceinline__ typename M::frag k_frag(const unsigned char *tile, int place, int row0, int blk, int st)
 {
     if constexpr (M::BF16) {
-        const u32x2_t a = *(const u32x2_t *)(tile + T::at(row, 4 * blk + (kg >> 1)) + 8 * (kg & 1));
-        const u32x2_t b = *(const u32x2_t *)(tile + T::at(row, 4 * blk + 2 + (kg >> 1)) + 8 * (kg & 1));
+        const u32x2_t a = *(const u32x2_t *)(tile + T::further(place, 4 * blk) + row0 * T::ROW);
+        const u32x2_t b = *(const u32x2_t *)(tile + T::further(place, 4 * blk + 2) + row0 * T::ROW);
         const u32x4_t u = {a[0], a[1], b[0], b[1]};
         return __builtin_bit_cast(bf16x8, u);
     } else {
-        return q_frag<M, T>(tile, row, blk, st, kg);
+        return q_frag<M, T>(tile, place, row0, blk, st);
     }
 }
-// ... and columns 16 c16 .. + 15, contraction over the 32 rows (tokens) of block `blk`.
+// ... and columns 16 c16 .. + 15, contraction over the 32 rows (tokens) of block `blk`. bf16: within 16 lanes, lane i supplies the
+// address of row i / 4 at columns 4 (i % 4) .. and receives four rows of its own column.
 template <class M, class T>
-__device__ __forceinline__ typename M::frag col_frag(const unsigned char *tile, int c16, int blk, int st, int lane)
+__device__ __forceinline__ int col_place(int lane)
 {
     const int kg = lane >> 4, i = lane & 15;
+    if constexpr (M::BF16) return T::at(4 * kg + (i >> 2), i >> 1 & 1) + 8 * (i & 1);
+    else return T::at(4 * kg, i >> 2) + 4 * (i & 3);
+}
+template <class M, class T>
+__device__ __forceinline__ typename M::frag col_frag(const unsigned char *tile, int place, int c16, int blk, int st)
+{
     if constexpr (M::BF16) {
-        // (within 16 lanes, lane i supplies the address of row i / 4 at columns 4 (i % 4) .. and receives four rows of its own column)
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef short s16x8 __attribute__((ext_vector_type(8)));
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const int row = 32 * blk + 4 * kg + (i >> 2);
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + T::at(row, 2 * c16 + (i >> 1 & 1)) + 8 * (i & 1)));
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + T::at(row + 16, 2 * c16 + (i >> 1 & 1)) + 8 * (i & 1)));
+        const unsigned char *p = tile + T::further(place, 2 * c16) + 32 * blk * T::ROW;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 16 * T::ROW));
         const s16x8 r = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
         return __builtin_bit_cast(bf16x8, r);
     } else {
-        const int row = 32 * blk + 16 * (st >> 2) + 4 * kg + (st & 3);
-        return *(const float *)(tile + T::at(row, 4 * c16 + (i >> 2)) + 4 * (i & 3));
+        return *(const float *)(tile + T::further(place, 4 * c16) + (32 * blk + 16 * (st >> 2) + (st & 3)) * T::ROW);
     }
 }
 
@@ -130,9 +170,9 @@ struct Shape {
     static constexpr int PK = (C * DK / E + NT - 1) / NT;     // pieces of a chunk's q or k rows per thread
     static constexpr int PV = C * 16 / E / 64;     // ... of its v rows
     static constexpr int UNITS = M::BF16 ? 6 : 2;  // (token block, 32 keys at or before it)
-    typedef Tile<DK, ES, 16> QT;
-    typedef Tile<DK, ES, M::BF16 ? 32 : 16> KT;
-    typedef Tile<16 * NW, ES, M::BF16 ? 32 : 16> VT;
+    typedef std::conditional_t<M::BF16, SwizzledTile16<DK>, PaddedTile16<DK, ES, 16>> QT;
+    typedef QT KT;
+    typedef PaddedTile16<16 * NW, ES, M::BF16 ? 32 : 16> VT;
     static constexpr size_t q_bytes = (size_t)C * QT::ROW, k_bytes = (size_t)C * KT::ROW, v_bytes = (size_t)C * VT::ROW;
     static constexpr size_t unit_bytes = M::STEPS * 64 * sizeof(typename M::frag);
     static constexpr size_t tables = 2 * 5 * 64 * sizeof(float);
@@ -303,6 +343,9 @@ void linear_walk_kernel(LinearWalkArgs a)
         }
     };
 
+    const int q_lane = q_place<QT>(lane), k_lane = k_place<M, KT>(lane), kt_lane = col_place<M, KT>(lane);
+    const int v_lane = VT::further(col_place<M, VT>(lane), w * (16 * ES / 16));
+
     // ---- decays: the last wave leaves those of the next chunk in the tables, lane j those of token j
     float gate = 1.0f, seg_decay = 1.0f;
     auto fetch_gate = [&](int c) {
@@ -383,6 +426,8 @@ void linear_walk_kernel(LinearWalkArgs a)
 
             if constexpr (!SUMMARY) {
                 // ---- masked products M[t, s] (k_s . q_t): a unit is a block of 16 tokens and 32 keys, left as operand fragments
+                const int k_at = anew(k_lane);
+                int q_at = anew(q_lane);
                 for (int unit = w; unit < SH::UNITS; unit += NW) {
                     const int tb = unit < 2 ? unit : 1 + unit / 2, sb = unit < 2 ? 0 : unit & 1;
                     f32x4 x[2];
@@ -394,8 +439,7 @@ void linear_walk_kernel(LinearWalkArgs a)
                         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                             for (int st = 0; st < STEPS; ++st)
-                                x[half] = M::mma(k_row_frag<M, KT>(sK, 32 * sb + 16 * half + n, kb, st, kg),
-                                                 q_frag<M, QT>(sQ, 16 * tb + n, kb, st, kg), x[half]);
+                                x[half] = M::mma(k_frag<M, KT>(sK, k_at, 32 * sb + 16 * half, kb, st), q_frag<M, QT>(sQ, q_at, 16 * tb, kb, st), x[half]);
                     }
                     // register r: key 32 sb + 16 half + 4 kg + r, token 16 tb + n
                     const float hi = sHi[16 * tb + n], lo = sLo[16 * tb + n];
@@ -419,6 +463,7 @@ void linear_walk_kernel(LinearWalkArgs a)
                 __builtin_amdgcn_sched_barrier(0);
 
                 // ---- zeta_t S_[n] q_t: pairs of the state's tiles are the A operand
+                q_at = anew(q_at);
                 if (GROUP == kQueries || s == 0) {
 #pragma unroll
                     for (int tb = 0; tb < TB; ++tb) y[tb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -432,7 +477,7 @@ void linear_walk_kernel(LinearWalkArgs a)
                             cut<M, PIECES>(x + VEC * st, f);
 #pragma unroll
                             for (int tb = 0; tb < TB; ++tb) {
-                                const frag qf = q_frag<M, QT>(sQ, 16 * tb + n, kb, st, kg);
+                                const frag qf = q_frag<M, QT>(sQ, q_at, 16 * tb, kb, st);
 #pragma unroll
                                 for (int i = 0; i < PIECES; ++i) y[tb] = M::mma(f[i], qf, y[tb]);
                             }
@@ -453,7 +498,7 @@ void linear_walk_kernel(LinearWalkArgs a)
 #pragma unroll
             for (int sb = 0; sb < SB; ++sb)
 #pragma unroll
-                for (int st = 0; st < STEPS; ++st) vt[sb][st] = col_frag<M, VT>(sV, w, sb, st, lane);
+                for (int st = 0; st < STEPS; ++st) vt[sb][st] = col_frag<M, VT>(sV, v_lane, 0, sb, st);
 
             if constexpr (!SUMMARY) {
                 // ---- + sum_s v_s M[t, s] (k_s . q_t)
@@ -533,6 +578,7 @@ void linear_walk_kernel(LinearWalkArgs a)
                 for (int j = 0; j < NJ; ++j) acc[j] *= zeta_C;
             }
             if (GROUP == kSources || s + 1 == steps) {
+                const int kt_at = anew(kt_lane);
 #pragma unroll
                 for (int sb = 0; sb < SB; ++sb) {
                     const f32x4 w0 = *(const f32x4 *)(sW + 32 * sb + 4 * kg), w1 = *(const f32x4 *)(sW + 32 * sb + 16 + 4 * kg);
@@ -547,7 +593,7 @@ void linear_walk_kernel(LinearWalkArgs a)
                         cut<M, VW>(x, f);
 #pragma unroll
                         for (int j = 0; j < NJ; ++j) {
-                            const frag kt = col_frag<M, KT>(sK, j, sb, st, lane);
+                            const frag kt = col_frag<M, KT>(sK, kt_at, j, sb, st);
 #pragma unroll
                             for (int i = 0; i < VW; ++i) acc[j] = M::mma(kt, f[i], acc[j]);
                         }
