@@ -417,6 +417,28 @@ __device__ __forceinline__ float sum_over_kg(float x)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// Sum over aligned groups of N lanes (a power of two), to all of them, by vector moves.
+template <int N>
+__device__ __forceinline__ float sum_over_lanes(float x)
+{
+    auto dpp_add = [](float v, auto ctrl) {
+        return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    if constexpr (N >= 2) x = dpp_add(x, std::integral_constant<int, 0xb1>{});    // quad_perm [1, 0, 3, 2]
+    if constexpr (N >= 4) x = dpp_add(x, std::integral_constant<int, 0x4e>{});    // quad_perm [2, 3, 0, 1]
+    if constexpr (N >= 8) x = dpp_add(x, std::integral_constant<int, 0x141>{});   // row_half_mirror
+    if constexpr (N >= 16) x = dpp_add(x, std::integral_constant<int, 0x140>{});  // row_mirror
+    if constexpr (N >= 32) {
+        const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    }
+    if constexpr (N >= 64) {
+        const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+    }
+    return x;
+}
+
 // log2(gamma) with the documented floor. Decays are kept in base-2 log space (the hardware's exp and log are
 // base 2): cumulative sums of these, and exp2 of their differences.
 __device__ __forceinline__ float log2_gate(float gamma) { return fmaxf(log2f(gamma), kMinLog2Gate); }

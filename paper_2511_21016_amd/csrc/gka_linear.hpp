@@ -68,10 +68,12 @@ struct LinearGateArgs {
     const float *gate;
     float *dgate;                 // [B, T, H_kv], or [H_kv] with gate_per_head
     int gate_per_head;
-    double *per_pair;             // [B, H_kv]: scratch with gate_per_head
     int B, T, Hkv;
+    double *part_sums, *per_part; // (carved from the workspace by the launcher)
+    int *part_open;
 };
-hipError_t launch_linear_gate(const LinearGateArgs &a, hipStream_t stream);
+size_t linear_gate_workspace_bytes(int64_t pairs, int T);
+hipError_t launch_linear_gate(const LinearGateArgs &a, void *workspace, hipStream_t stream);
 hipError_t launch_linear_state_sum(const float *per_sequence, float *out, int groups, int share, int64_t state_floats,
                                    hipStream_t stream);
 

@@ -132,7 +132,7 @@ gka::LinearWalkArgs walk_args(const gka_linear_params *p, const Sizes &s, const 
 struct BackwardPlan {
     Sizes s;
     WalkPlan q, k, v;                  // the walks of dq, dk, dv
-    size_t off_q_dot, off_k_dot, off_state_dot, off_pair, off_states, total;
+    size_t off_q_dot, off_k_dot, off_state_dot, off_gate, off_states, total;
 };
 
 gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
@@ -149,7 +149,7 @@ gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
     b->off_q_dot = off; off += align_up(b->q.shape.slices * tokens * b->s.G * sizeof(float), 256);
     b->off_k_dot = off; off += align_up(b->k.shape.slices * tokens * sizeof(float), 256);
     b->off_state_dot = off; off += align_up(b->q.shape.slices * b->s.pairs * sizeof(float), 256);
-    b->off_pair = off; off += align_up(b->s.pairs * sizeof(double), 256);
+    b->off_gate = off; off += align_up(gka::linear_gate_workspace_bytes(b->s.pairs, p->T), 256);
     b->off_states = off;
     // (room for a state of every sequence whether or not initial states are shared: one size for all calls)
     off += align_up((size_t)b->s.pairs * p->d_k * p->d_v * sizeof(float), 256);
@@ -278,9 +278,8 @@ gka_status gka_linear_backward(const gka_linear_params *p, const void *q, const 
     g.q_dq = q_dot; g.k_dk = k_dot; g.state_dot = dS_final ? state_dot : nullptr;
     g.q_slices = b.q.shape.slices; g.k_slices = b.k.shape.slices; g.G = s.G;
     g.gate = gate; g.dgate = dgate; g.gate_per_head = p->gate_per_head;
-    g.per_pair = (double *)(ws + b.off_pair);
     g.B = p->B; g.T = p->T; g.Hkv = p->H_kv;
-    return gka::launch_linear_gate(g, stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
+    return gka::launch_linear_gate(g, ws + b.off_gate, stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
 }
 
 gka_status gka_linear_decode(const gka_linear_params *p, const float *S_in, float *S_out, const void *q, const void *k, const void *v,

@@ -15,18 +15,27 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 // ---- decode ----------------------------------------------------------------------------------------------------------
 // A row of the state (one v-feature) lies across LPR lanes, four k-features on each; a thread holds NR rows, a workgroup
-// (256 / LPR) NR of them. The state crosses memory once, whatever the number of tokens.
+// (256 / LPR) NR of them. The state crosses memory once, whatever the number of tokens. Rows of q, k, v and gates come through LDS, as
+// many tokens at a time as fit, so that their latency is paid once and beside the state's.
+constexpr int kDecodeQueries = 32;                 // q rows of a pass through LDS, or those of one token in parts of as many
+constexpr int kDecodeTokens = 16;                  // tokens of a pass at most
+
 template <bool BF16, int LPR, int NR>
-__global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a)
+__global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a, int tokens)
 {
     typedef std::conditional_t<BF16, IOBF16, IOF32> IO;
     typedef typename IO::type elem_t;
     constexpr int RP = 256 / LPR;                  // rows a workgroup covers at once
+    constexpr int DKP = 4 * LPR;                   // k-features with padding
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const int queries = a.G < kDecodeQueries ? a.G : kDecodeQueries;       // heads of a token in LDS at once
+    float *sk = lds, *sv = sk + tokens * DKP, *sg = sv + tokens * RP * NR, *sq = sg + kDecodeTokens;
     const int blocks = (a.dv + RP * NR - 1) / (RP * NR);
     const int64_t pair = blockIdx.x / blocks;
-    const int row0 = (int)(blockIdx.x % blocks) * RP * NR + (int)(threadIdx.x / LPR);
+    const int row_first = (int)(blockIdx.x % blocks) * RP * NR;
+    const int tid = threadIdx.x, row0 = row_first + tid / LPR;
     const int b = (int)(pair / a.Hkv), h = (int)(pair % a.Hkv);
-    const int l = threadIdx.x % LPR, col = 4 * l;
+    const int l = tid % LPR, col = 4 * l;
     const bool col_in = col < a.dk;
     const float *S0 = a.S_in + ((int64_t)(b / a.share) * a.Hkv + h) * a.dv * a.dk;
     f32x4 S[NR];
@@ -35,49 +44,58 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a)
         const int row = row0 + i * RP;
         S[i] = col_in && row < a.dv ? *(const f32x4 *)(S0 + (int64_t)row * a.dk + col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    for (int t = 0; t < a.T; ++t) {
-        const elem_t *k = (const elem_t *)a.k.p + b * a.k.sb + t * a.k.st + h * a.k.sh;
-        const elem_t *v = (const elem_t *)a.v.p + b * a.v.sb + t * a.v.st + h * a.v.sh;
-        const float gate = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + t) * a.Hkv + h];
-        const f32x4 k4 = col_in ? IO::load4(k, col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            const int row = row0 + i * RP;
-            const float x = row < a.dv ? IO::load(v, row) : 0.0f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) S[i][e] = gate * S[i][e] + x * k4[e];
+    auto row_of = [&](const RowTensor &x, int t, int head) { return (const elem_t *)x.p + b * x.sb + t * x.st + head * x.sh; };
+    // q rows of `heads` heads from `head0` on of tokens t0 .. t0 + count - 1
+    auto load_q = [&](int t0, int count, int head0, int heads) {
+        for (int i = tid / LPR; i < count * heads; i += RP)
+            *(f32x4 *)(sq + i * DKP + col) = col_in ? IO::load4(row_of(a.q, t0 + i / heads, h * a.G + head0 + i % heads), col)
+                                                    : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    for (int t0 = 0; t0 < a.T; t0 += tokens) {
+        const int count = a.T - t0 < tokens ? a.T - t0 : tokens;
+        if (t0 > 0) __syncthreads();
+        for (int i = tid / LPR; i < count; i += RP)
+            *(f32x4 *)(sk + i * DKP + col) = col_in ? IO::load4(row_of(a.k, t0 + i, h), col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = tid; i < count * RP * NR; i += 256) {
+            const int row = row_first + i % (RP * NR);
+            sv[i] = row < a.dv ? IO::load(row_of(a.v, t0 + i / (RP * NR), h), row) : 0.0f;
         }
-        for (int s = 0; s < a.G; ++s) {
-            const int head = h * a.G + s;
-            const elem_t *q = (const elem_t *)a.q.p + b * a.q.sb + t * a.q.st + head * a.q.sh;
-            elem_t *y = (elem_t *)const_cast<void *>(a.y.p) + b * a.y.sb + t * a.y.st + head * a.y.sh;
-            const f32x4 q4 = col_in ? IO::load4(q, col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            float p[NR];
+        if (tid < count) sg[tid] = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + t0 + tid) * a.Hkv + h];
+        load_q(t0, count, 0, queries);
+        __syncthreads();
+        for (int t = 0; t < count; ++t) {
+            const float gate = sg[t];
+            const f32x4 k4 = *(const f32x4 *)(sk + t * DKP + col);
 #pragma unroll
-            for (int i = 0; i < NR; ++i) p[i] = (S[i][0] * q4[0] + S[i][1] * q4[1]) + (S[i][2] * q4[2] + S[i][3] * q4[3]);
-            // sums over the LPR lanes of a row: while a lane holds several rows, the two lanes of an exchange keep a half each
-            int n = NR;
+            for (int i = 0; i < NR; ++i) {
+                const float x = sv[t * RP * NR + i * RP + tid / LPR];
 #pragma unroll
-            for (int off = LPR / 2; off > 0; off >>= 1) {
-                if (n > 1) {
-                    const bool upper = (l & off) != 0;
-#pragma unroll
-                    for (int i = 0; i < NR / 2; ++i) {
-                        if (i >= n / 2) break;
-                        const float send = upper ? p[i] : p[i + n / 2], keep = upper ? p[i + n / 2] : p[i];
-                        p[i] = keep + __shfl_xor(send, off, 64);
-                    }
-                    n /= 2;
-                } else {
-                    p[0] += __shfl_xor(p[0], off, 64);
-                }
+                for (int e = 0; e < 4; ++e) S[i][e] = gate * S[i][e] + x * k4[e];
             }
-            constexpr int HELD = NR > LPR ? NR / LPR : 1, TWINS = NR > LPR ? 1 : LPR / NR;   // rows a lane holds, lanes that hold a row
-            if (l % TWINS == 0) {
+            for (int head0 = 0; head0 < a.G; head0 += queries) {
+                const int heads = a.G - head0 < queries ? a.G - head0 : queries;
+                if (head0 > 0 || (a.G > queries && t > 0)) {               // (more heads than LDS has room for: part by part)
+                    __syncthreads();
+                    load_q(t0 + t, 1, head0, heads);
+                    __syncthreads();
+                }
+                const float *q = sq + (a.G > queries ? 0 : t * queries) * DKP + col;
+                for (int s = 0; s < heads; ++s) {
+                    const f32x4 q4 = *(const f32x4 *)(q + s * DKP);
+                    float mine = 0.0f;                     // lane i of the LPR: row i (i < NR), lanes of other NR the same again
 #pragma unroll
-                for (int i = 0; i < HELD; ++i) {
-                    const int row = row0 + (l / TWINS * HELD + i) * RP;
-                    if (row < a.dv) IO::store1(y, row, p[i]);
+                    for (int i = 0; i < NR; ++i) {
+                        const float p = sum_over_lanes<LPR>((S[i][0] * q4[0] + S[i][1] * q4[1]) + (S[i][2] * q4[2] + S[i][3] * q4[3]));
+                        if (LPR >= NR) mine = l == i ? p : mine;
+                        else if (l == i % LPR) {
+                            const int row = row0 + i * RP;
+                            if (row < a.dv) IO::store1(const_cast<elem_t *>(row_of(a.y, t0 + t, h * a.G + head0 + s)), row, p);
+                        }
+                    }
+                    if (LPR >= NR && l < NR) {
+                        const int row = row0 + l * RP;
+                        if (row < a.dv) IO::store1(const_cast<elem_t *>(row_of(a.y, t0 + t, h * a.G + head0 + s)), row, mine);
+                    }
                 }
             }
         }
@@ -91,24 +109,25 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a)
 }
 
 // ---- shared ----------------------------------------------------------------------------------------------------------
-// A workgroup takes up to `ncol` columns of one (prefix, kv head): a column is a query head of a sequence, G of them to a
-// sequence, one behind the other. First S q of all its columns on the matrix cores (S cut into two bf16 pieces, or float32),
-// then each wave the cached tokens of its columns, up to four of one sequence at a time.
-constexpr int kSharedCols = 32, kSharedHeads = 4;
+// A workgroup takes up to 16 columns of one (prefix, kv head): a column is a query head of a sequence, G of them to a
+// sequence, one behind the other. First S q of its columns on the matrix cores (16 x 16 tiles: 16 rows of S to a wave; S cut into
+// two bf16 pieces, or float32), then each wave the cached tokens of its columns, up to four of one sequence at a time, LR lanes to
+// a row of 16-byte pieces.
+constexpr int kSharedCols = 16, kSharedHeads = 4, kSharedWaves = 8;
 
-template <bool BF16>
-__global__ __launch_bounds__(256) void linear_shared_kernel(LinearSharedArgs a, int ncol, int lk, int lv)
+template <bool BF16, int LR>
+__global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(LinearSharedArgs a, int ncol)
 {
     typedef std::conditional_t<BF16, IOBF16, IOF32> IO;
     typedef typename IO::type elem_t;
     constexpr int E = BF16 ? 8 : 4;                // elements of a 16-byte piece
+    constexpr int RP = 64 / LR;                    // rows a wave reads at once
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int ys = a.dv + 4;                       // floats of a column of S q
     float *sY = (float *)smem;
     float *sS = sY + ncol * ys;                    // [waves][kSharedHeads][64]
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 31, g = lane >> 5;
     const int64_t cols = (int64_t)a.share * a.G;
     const int tiles = (int)((cols + ncol - 1) / ncol);
     const int tile = blockIdx.x % tiles;
@@ -119,54 +138,59 @@ __global__ __launch_bounds__(256) void linear_shared_kernel(LinearSharedArgs a, 
     const float *S = a.S + ((int64_t)prefix * a.Hkv + h) * a.dv * a.dk;
     auto row_of = [&](const RowTensor &x, int b, int head) { return (const elem_t *)x.p + b * x.sb + head * x.sh; };
 
-    // ---- S q: wave w takes the 32-row blocks w, w + 4, ..
+    // ---- S q: wave w takes the rows 16 w .. + 15, 16 (w + 8) .. + 15
     {
-        const int c = n < my_cols ? n : 0;         // (columns that do not exist repeat the first; their results are not read)
+        const int n = lane & 15, kg = lane >> 4;
+        const int c = n < my_cols ? n : 0;         // (columns that do not exist repeat the first; their results are not kept)
         const int64_t col = col0 + c;
         const elem_t *q = row_of(a.q, prefix * a.share + (int)(col / a.G), h * a.G + (int)(col % a.G));
-        for (int rb = w; 32 * rb < a.dv; rb += 4) {
-            f32x16 acc = zero16();
-            const int row = 32 * rb + n;
-            const bool in = row < a.dv;
-            const float *s = S + (int64_t)(in ? row : 0) * a.dk;
-            if constexpr (BF16) {
-#pragma unroll 4
-                for (int k0 = 0; k0 < a.dk; k0 += 16) {
-                    const f32x4 x0 = *(const f32x4 *)(s + k0 + 8 * g), x1 = *(const f32x4 *)(s + k0 + 8 * g + 4);
-                    const u32x4_t qv = *(const u32x4_t *)(q + k0 + 8 * g);
-                    float x[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]}, back[8];
-                    const bf16x8 hi = MmaBF16::pack(x), qf = __builtin_bit_cast(bf16x8, qv);
-                    MmaBF16::unpack(hi, back);
+        for (int rb = w; 16 * rb < a.dv; rb += kSharedWaves) {
+            f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+            const float *s = S + (int64_t)(16 * rb + n) * a.dk;
+            // 32 k-features a step, four steps' rows in flight (features that do not exist: zeros on both sides)
+            constexpr int KSTEPS = E * LR / 32 > 0 ? E * LR / 32 : 1, FLY = KSTEPS < 4 ? KSTEPS : 4;
+            const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int s0 = 0; s0 < KSTEPS; s0 += FLY) {
+                f32x4 x0[FLY], x1[FLY];
+                u32x4_t q0[FLY], q1[FLY];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] -= back[e];
-                    acc = MmaBF16::mma(hi, qf, acc);
-                    acc = MmaBF16::mma(MmaBF16::pack(x), qf, acc);
+                for (int i = 0; i < FLY; ++i) {
+                    const int k0 = 32 * (s0 + i) + 8 * kg;
+                    const bool in = k0 < a.dk;
+                    x0[i] = in ? *(const f32x4 *)(s + k0) : zero;
+                    x1[i] = in ? *(const f32x4 *)(s + k0 + 4) : zero;
+                    q0[i] = in ? *(const u32x4_t *)(q + k0) : u32x4_t{0, 0, 0, 0};
+                    if constexpr (!BF16) q1[i] = in ? *(const u32x4_t *)(q + k0 + 4) : u32x4_t{0, 0, 0, 0};
                 }
-            } else {
-#pragma unroll 4
-                for (int k0 = 0; k0 < a.dk; k0 += 8) {
-                    const f32x4 x = *(const f32x4 *)(s + k0 + 4 * g), qv = *(const f32x4 *)(q + k0 + 4 * g);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc = MmaF32::mma(x[e], qv[e], acc);
+                for (int i = 0; i < FLY; ++i) {
+                    if constexpr (BF16) {
+                        float x[8] = {x0[i][0], x0[i][1], x0[i][2], x0[i][3], x1[i][0], x1[i][1], x1[i][2], x1[i][3]}, back[8];
+                        const bf16x8 hi = MmaBF16::pack(x), qf = __builtin_bit_cast(bf16x8, q0[i]);
+                        MmaBF16::unpack(hi, back);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] -= back[e];
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, qf, acc, 0, 0, 0);
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(MmaBF16::pack(x), qf, acc, 0, 0, 0);
+                    } else {
+                        const f32x4 qa = __builtin_bit_cast(f32x4, q0[i]), qb = __builtin_bit_cast(f32x4, q1[i]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x0[i][e], qa[e], acc, 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x1[i][e], qb[e], acc, 0, 0, 0);
+                    }
                 }
             }
-            if (n < my_cols) {
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4)
-                    if (32 * rb + 8 * q4 < a.dv)
-                        *(f32x4 *)(sY + n * ys + 32 * rb + 8 * q4 + 4 * g) =
-                            f32x4{acc[4 * q4], acc[4 * q4 + 1], acc[4 * q4 + 2], acc[4 * q4 + 3]};
-            }
+            if (n < my_cols) *(f32x4 *)(sY + n * ys + 16 * rb + 4 * kg) = acc;
         }
     }
     __syncthreads();
 
     // ---- the cached tokens
     float *score = sS + w * kSharedHeads * 64;
-    const int kl = lane % lk, kr = lane / lk, krows = 64 / lk;     // pieces of a key row across lk lanes
-    const int vl = lane % lv, vr = lane / lv, vrows = 64 / lv;
-    const bool k_in = E * kl < a.dk, v_in = E * vl < a.dv;
-    const int per_wave = (ncol + 3) / 4;
+    const int l = lane % LR, r = lane / LR;        // piece of a row, row of a read
+    const bool k_in = E * l < a.dk, v_in = E * l < a.dv;
+    const int per_wave = (ncol + kSharedWaves - 1) / kSharedWaves;
     int c = w * per_wave;
     const int c_end = c + per_wave < my_cols ? c + per_wave : my_cols;
     while (c < c_end) {
@@ -186,8 +210,8 @@ __global__ __launch_bounds__(256) void linear_shared_kernel(LinearSharedArgs a, 
         elem_t *kc = (elem_t *)a.k_cache + cache_row * a.dk, *vc = (elem_t *)a.v_cache + cache_row * a.dv;
         const int64_t kc_step = (int64_t)a.Hkv * a.dk, vc_step = (int64_t)a.Hkv * a.dv;
         if (head0 == 0) {                          // (once for a sequence: the new token goes into the cache)
-            if (kr == 0 && k_in) *(u32x4_t *)(kc + len * kc_step + E * kl) = *(const u32x4_t *)(k_new + E * kl);
-            if (vr == 0 && v_in) *(u32x4_t *)(vc + len * vc_step + E * vl) = *(const u32x4_t *)(v_new + E * vl);
+            if (r == 0 && k_in) *(u32x4_t *)(kc + len * kc_step + E * l) = *(const u32x4_t *)(k_new + E * l);
+            if (r == 0 && v_in) *(u32x4_t *)(vc + len * vc_step + E * l) = *(const u32x4_t *)(v_new + E * l);
             if (!a.gate_per_head && lane == 0) a.gate_cache[cache_row + (int64_t)len * a.Hkv] = gate_new;
         }
         float q[kSharedHeads][E], y[kSharedHeads][E];
@@ -198,11 +222,26 @@ __global__ __launch_bounds__(256) void linear_shared_kernel(LinearSharedArgs a, 
             for (int e = 0; e < E; ++e) y[i][e] = 0.0f;
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
-                const f32x4 x = k_in ? IO::load4(row, E * kl + e) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                const f32x4 x = k_in ? IO::load4(row, E * l + e) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) q[i][e + j] = x[j];
             }
         }
+        // a row's piece as floats (zeros: not one of the tile's tokens, or beyond the features)
+        typedef struct { u32x4_t bits; } piece;
+        auto fetch = [&](const elem_t *cache, int64_t step, const elem_t *newest, int j, bool in) {
+            return piece{in ? *(const u32x4_t *)((j < len ? cache + j * step : newest) + E * l) : u32x4_t{0, 0, 0, 0}};
+        };
+        auto floats = [](piece p, float (&x)[E]) {
+            if constexpr (BF16) {
+                MmaBF16::unpack(__builtin_bit_cast(bf16x8, p.bits), x);
+            } else {
+                const f32x4 u = __builtin_bit_cast(f32x4, p.bits);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = u[e];
+            }
+        };
+        constexpr int FLY = LR < 8 ? LR : 8;       // reads in flight
         double behind = 0.0;                       // log2 decay over the tokens behind the tile
         for (int j0 = len / 64 * 64; j0 >= 0; j0 -= 64) {
             const int count = len + 1 - j0 < 64 ? len + 1 - j0 : 64;
@@ -211,72 +250,69 @@ __global__ __launch_bounds__(256) void linear_shared_kernel(LinearSharedArgs a, 
                 const float gate = a.gate_per_head || j0 + lane == len ? gate_new : a.gate_cache[cache_row + (int64_t)(j0 + lane) * a.Hkv];
                 lg = (double)log2_gate(gate);
             }
-            const double G = wave_inclusive_scan_f64(lg), total = lane63_f64(G);
-            const float weight = lane < count ? exp2f((float)(behind + (total - G))) : 0.0f;
-            behind += total;
-#pragma unroll 4
-            for (int r = 0; r < count; r += krows) {
-                const int j = j0 + r + kr;
-                const elem_t *row = j < len ? kc + j * kc_step : k_new;
-                const bool in = k_in && r + kr < count;
-                float x[E];
+            for (int s0 = 0; s0 < count; s0 += FLY * RP) {
+                piece p[FLY];
 #pragma unroll
-                for (int e = 0; e < E; e += 4) {
-                    const f32x4 u = in ? IO::load4(row, E * kl + e) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int i = 0; i < FLY; ++i) p[i] = fetch(kc, kc_step, k_new, j0 + s0 + i * RP + r, k_in && s0 + i * RP + r < count);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[e + i] = u[i];
-                }
+                for (int i = 0; i < FLY; ++i) {
+                    float x[E];
+                    floats(p[i], x);
 #pragma unroll
-                for (int i = 0; i < kSharedHeads; ++i) {
-                    if (i >= m) break;
-                    float dot = 0.0f;
+                    for (int g = 0; g < kSharedHeads; ++g) {
+                        if (g < m) {
+                            float dot = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) dot += x[e] * q[i][e];
-                    for (int off = lk / 2; off > 0; off >>= 1) dot += __shfl_xor(dot, off, 64);
-                    if (kl == 0 && r + kr < 64) score[i * 64 + r + kr] = dot;
+                            for (int e = 0; e < E; ++e) dot += x[e] * q[g][e];
+                            dot = sum_over_lanes<LR>(dot);
+                            if (l == 0) score[g * 64 + s0 + i * RP + r] = dot;
+                        }
+                    }
                 }
             }
+            const double G = wave_inclusive_scan_f64(lg), total = lane63_f64(G);
+            const float weight = lane < count ? __builtin_amdgcn_exp2f((float)(behind + (total - G))) : 0.0f;
+            behind += total;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the wave's own scores)
 #pragma unroll
-            for (int i = 0; i < kSharedHeads; ++i)
-                if (i < m) score[i * 64 + lane] = lane < count ? score[i * 64 + lane] * weight : 0.0f;
+            for (int g = 0; g < kSharedHeads; ++g)
+                if (g < m) score[g * 64 + lane] = lane < count ? score[g * 64 + lane] * weight : 0.0f;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll 4
-            for (int r = 0; r < count; r += vrows) {
-                const int j = j0 + r + vr;
-                const elem_t *row = j < len ? vc + j * vc_step : v_new;
-                const bool in = v_in && r + vr < count;
-                float x[E];
+            for (int s0 = 0; s0 < count; s0 += FLY * RP) {
+                piece p[FLY];
 #pragma unroll
-                for (int e = 0; e < E; e += 4) {
-                    const f32x4 u = in ? IO::load4(row, E * vl + e) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int i = 0; i < FLY; ++i) p[i] = fetch(vc, vc_step, v_new, j0 + s0 + i * RP + r, v_in && s0 + i * RP + r < count);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[e + i] = u[i];
-                }
+                for (int i = 0; i < FLY; ++i) {
+                    float x[E];
+                    floats(p[i], x);
 #pragma unroll
-                for (int i = 0; i < kSharedHeads; ++i) {
-                    if (i >= m) break;
-                    const float s = score[i * 64 + ((r + vr) & 63)];
+                    for (int g = 0; g < kSharedHeads; ++g) {
+                        if (g < m) {
+                            const float s = score[g * 64 + s0 + i * RP + r];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) y[i][e] += s * x[e];
+                            for (int e = 0; e < E; ++e) y[g][e] += s * x[e];
+                        }
+                    }
                 }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (read before the next tile's are written)
         }
-        const float zeta = exp2f((float)behind);
+        const float zeta = __builtin_amdgcn_exp2f((float)behind);
 #pragma unroll
-        for (int i = 0; i < kSharedHeads; ++i) {
-            if (i >= m) break;
+        for (int g = 0; g < kSharedHeads; ++g) {
+            if (g >= m) continue;
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                for (int off = lv; off < 64; off <<= 1) y[i][e] += __shfl_xor(y[i][e], off, 64);
-            if (vr == 0 && v_in) {
-                elem_t *out = const_cast<elem_t *>(row_of(a.y, b, h * a.G + head0 + i)) + E * vl;
-                const float *s = sY + (c + i) * ys + E * vl;
+#pragma unroll
+                for (int off = LR; off < 64; off <<= 1) y[g][e] += __shfl_xor(y[g][e], off, 64);
+            if (r == 0 && v_in) {
+                elem_t *out = const_cast<elem_t *>(row_of(a.y, b, h * a.G + head0 + g)) + E * l;
+                const float *s = sY + (c + g) * ys + E * l;
 #pragma unroll
                 for (int e = 0; e < E; e += 4)
-                    IO::store4(out, e, zeta * s[e] + y[i][e], zeta * s[e + 1] + y[i][e + 1], zeta * s[e + 2] + y[i][e + 2],
-                               zeta * s[e + 3] + y[i][e + 3]);
+                    IO::store4(out, e, zeta * s[e] + y[g][e], zeta * s[e + 1] + y[g][e + 1], zeta * s[e + 2] + y[g][e + 2],
+                               zeta * s[e + 3] + y[g][e + 3]);
             }
         }
         c += m;
@@ -290,6 +326,19 @@ int pow2_at_least(int x)
     return p;
 }
 
+template <bool BF16, int LPR, int NR>
+hipError_t launch_decode_kernel(const LinearDecodeArgs &a, int64_t blocks, hipStream_t stream)
+{
+    // tokens of a pass through LDS: as many as all of whose q rows have room
+    int tokens = a.G >= kDecodeQueries ? 1 : kDecodeQueries / a.G;
+    tokens = tokens < kDecodeTokens ? tokens : kDecodeTokens;
+    tokens = tokens < a.T ? tokens : a.T;
+    const int queries = a.G < kDecodeQueries ? tokens * a.G : kDecodeQueries;
+    const size_t lds = ((size_t)(tokens + queries) * 4 * LPR + tokens * (256 / LPR) * NR + kDecodeTokens) * sizeof(float);
+    hipLaunchKernelGGL((linear_decode_kernel<BF16, LPR, NR>), dim3((unsigned)blocks), dim3(256), lds, stream, a, tokens);
+    return hipGetLastError();
+}
+
 template <bool BF16, int LPR>
 hipError_t launch_decode_rows(const LinearDecodeArgs &a, hipStream_t stream)
 {
@@ -297,13 +346,9 @@ hipError_t launch_decode_rows(const LinearDecodeArgs &a, hipStream_t stream)
     const int64_t pairs = (int64_t)a.B * a.Hkv;
     // as many rows to a thread as leave four workgroups to a CU
     const auto blocks = [&](int nr) { return pairs * ((a.dv + RP * nr - 1) / (RP * nr)); };
-    if (blocks(8) >= 1024)
-        hipLaunchKernelGGL((linear_decode_kernel<BF16, LPR, 8>), dim3((unsigned)blocks(8)), dim3(256), 0, stream, a);
-    else if (blocks(4) >= 1024)
-        hipLaunchKernelGGL((linear_decode_kernel<BF16, LPR, 4>), dim3((unsigned)blocks(4)), dim3(256), 0, stream, a);
-    else
-        hipLaunchKernelGGL((linear_decode_kernel<BF16, LPR, 1>), dim3((unsigned)blocks(1)), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    if (blocks(8) >= 1024) return launch_decode_kernel<BF16, LPR, 8>(a, blocks(8), stream);
+    if (blocks(4) >= 1024) return launch_decode_kernel<BF16, LPR, 4>(a, blocks(4), stream);
+    return launch_decode_kernel<BF16, LPR, 1>(a, blocks(1), stream);
 }
 
 template <bool BF16>
@@ -318,6 +363,33 @@ hipError_t launch_decode(const LinearDecodeArgs &a, hipStream_t stream)
     }
 }
 
+template <bool BF16, int LR>
+hipError_t launch_shared(const LinearSharedArgs &a, hipStream_t stream)
+{
+    const int64_t cols = (int64_t)a.share * a.G, groups = (int64_t)(a.B / a.share) * a.Hkv;
+    // two workgroups to a CU, with fewer columns to each where there are not so many
+    int ncol = kSharedCols;
+    while (ncol > 1 && groups * ((cols + ncol - 1) / ncol) < 512) ncol /= 2;
+    const int64_t blocks = groups * ((cols + ncol - 1) / ncol);
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const size_t lds = ((size_t)ncol * (a.dv + 4) + kSharedWaves * kSharedHeads * 64) * sizeof(float);
+    hipLaunchKernelGGL((linear_shared_kernel<BF16, LR>), dim3((unsigned)blocks), dim3(64 * kSharedWaves), lds, stream, a, ncol);
+    return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t launch_shared_rows(const LinearSharedArgs &a, hipStream_t stream)
+{
+    switch (pow2_at_least((a.dk > a.dv ? a.dk : a.dv) / (BF16 ? 8 : 4))) {
+    case 2: if constexpr (BF16) return launch_shared<true, 2>(a, stream); else return hipErrorInvalidValue;
+    case 4: return launch_shared<BF16, 4>(a, stream);
+    case 8: return launch_shared<BF16, 8>(a, stream);
+    case 16: return launch_shared<BF16, 16>(a, stream);
+    case 32: return launch_shared<BF16, 32>(a, stream);
+    default: if constexpr (!BF16) return launch_shared<false, 64>(a, stream); else return hipErrorInvalidValue;
+    }
+}
+
 }  // namespace
 
 hipError_t launch_linear_decode(const LinearDecodeArgs &a, bool bf16, hipStream_t stream)
@@ -327,20 +399,7 @@ hipError_t launch_linear_decode(const LinearDecodeArgs &a, bool bf16, hipStream_
 
 hipError_t launch_linear_shared(const LinearSharedArgs &a, bool bf16, hipStream_t stream)
 {
-    const int e = bf16 ? 8 : 4;
-    const int64_t cols = (int64_t)a.share * a.G, groups = (int64_t)(a.B / a.share) * a.Hkv;
-    int ncol = kSharedCols;
-    while (ncol > 4 && groups * ((cols + ncol - 1) / ncol) < 512) ncol /= 2;
-    const int64_t blocks = groups * ((cols + ncol - 1) / ncol);
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const size_t lds = ((size_t)ncol * (a.dv + 4) + 4 * kSharedHeads * 64) * sizeof(float);
-    if (bf16)
-        hipLaunchKernelGGL(linear_shared_kernel<true>, dim3((unsigned)blocks), dim3(256), lds, stream, a, ncol, pow2_at_least(a.dk / e),
-                           pow2_at_least(a.dv / e));
-    else
-        hipLaunchKernelGGL(linear_shared_kernel<false>, dim3((unsigned)blocks), dim3(256), lds, stream, a, ncol, pow2_at_least(a.dk / e),
-                           pow2_at_least(a.dv / e));
-    return hipGetLastError();
+    return bf16 ? launch_shared_rows<true>(a, stream) : launch_shared_rows<false>(a, stream);
 }
 
 }  // namespace gka

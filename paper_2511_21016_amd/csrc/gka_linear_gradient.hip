@@ -9,76 +9,108 @@ namespace {
 // dL/dlog(gate_t) is what the tokens from t on read of the states before t:
 //   L_t = x_t + L_{t+1},  x_t = sum_g q_t . dq_t - k_t . dk_t,  L_T = <dS_final, S_T>;   dgate_t = L_t / gate_t.
 // A gate of at most exp(-100) wipes the state (L_t = 0 there): the sum starts anew before it and its own gradient is
-// written as 0. One workgroup to a (sequence, kv head): a thread sums a run of consecutive tokens, runs are joined by a scan
-// over the threads, all in float64.
-constexpr int kThreads = 256;
+// written as 0. A workgroup takes up to 4096 tokens of a (sequence, kv head), four consecutive ones to a thread, joined by a scan over
+// the threads in float64; of longer sequences a first launch (SUMS) leaves what each part adds up to.
+constexpr int kThreads = 1024, kRun = 4, kPart = kThreads * kRun;
+constexpr float kWiped = 3.8e-44f;                 // exp(-100) to float32's last bits there
+
+template <bool SUMS>
 __global__ __launch_bounds__(kThreads) void linear_gate_kernel(LinearGateArgs a)
 {
-    __shared__ double sum[2][kThreads];
-    __shared__ int open[2][kThreads];
-    const int pair = blockIdx.x, n_pairs = a.B * a.Hkv;
+    // a run of tokens takes what comes from behind it, c, to sum + (open ? c : 0)
+    __shared__ double wave_sums[kThreads / 64];
+    __shared__ int wave_open[kThreads / 64];
+    const int pair = blockIdx.x % (a.B * a.Hkv), part = blockIdx.x / (a.B * a.Hkv), n_pairs = a.B * a.Hkv;
+    const int parts = (a.T + kPart - 1) / kPart;
     const int b = pair / a.Hkv, h = pair % a.Hkv;
-    const int tid = threadIdx.x;
-    const int run = (a.T + kThreads - 1) / kThreads;
-    const int t0 = min(tid * run, a.T), t1 = min(t0 + run, a.T);
-    const float wiped = 3.8e-44f;                  // exp(-100) to float32's last bits there
-    auto gate_at = [&](int t) { return a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + t) * a.Hkv + h]; };
-    auto x_at = [&](int t) {
-        double x = 0.0;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int t0 = part * kPart + tid * kRun;
+    float gate[kRun];
+    double x[kRun];
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+        const int t = t0 + i;
+        gate[i] = 1.0f;
+        x[i] = 0.0;
+        if (t >= a.T) continue;
+        gate[i] = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + t) * a.Hkv + h];
         for (int s = 0; s < a.q_slices; ++s)
-            for (int i = 0; i < a.G; ++i) x += (double)a.q_dq[(((int64_t)s * n_pairs + pair) * a.G + i) * a.T + t];
-        for (int s = 0; s < a.k_slices; ++s) x -= (double)a.k_dk[((int64_t)s * n_pairs + pair) * a.T + t];
-        return x;
-    };
-    // a run takes what comes from behind, c, to sum + (open ? c : 0)
-    double mine = 0.0;
-    int mine_open = 1;
-    for (int t = t1 - 1; t >= t0; --t) {
-        mine += x_at(t);
-        if (!(gate_at(t) > wiped)) {
-            mine = 0.0;
-            mine_open = 0;
+            for (int g = 0; g < a.G; ++g) x[i] += (double)a.q_dq[(((int64_t)s * n_pairs + pair) * a.G + g) * a.T + t];
+        for (int s = 0; s < a.k_slices; ++s) x[i] -= (double)a.k_dk[((int64_t)s * n_pairs + pair) * a.T + t];
+    }
+    double sum = 0.0;
+    int open = 1;
+#pragma unroll
+    for (int i = kRun - 1; i >= 0; --i) {
+        sum += x[i];
+        if (!(gate[i] > kWiped)) {
+            sum = 0.0;
+            open = 0;
         }
     }
-    sum[0][tid] = mine;
-    open[0][tid] = mine_open;
+    // this thread's run with those of the threads behind it in the wave
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+        const double s = __shfl_down(sum, off, 64);
+        const int o = __shfl_down(open, off, 64);
+        if (lane + off < 64 && open) {
+            sum += s;
+            open = o;
+        }
+    }
+    if (lane == 0) {
+        wave_sums[w] = sum;
+        wave_open[w] = open;
+    }
     __syncthreads();
-    int from = 0;
-    for (int off = 1; off < kThreads; off *= 2) {
-        double s = sum[from][tid];
-        int o = open[from][tid];
-        if (o && tid + off < kThreads) {
-            s += sum[from][tid + off];
-            o = open[from][tid + off];
+    if constexpr (SUMS) {
+        if (tid == 0) {
+            double all = 0.0;
+            int through = 1;
+            for (int i = kThreads / 64 - 1; i >= 0; --i) {
+                all = wave_sums[i] + (wave_open[i] ? all : 0.0);
+                through &= wave_open[i];
+            }
+            a.part_sums[(int64_t)pair * parts + part] = all;
+            a.part_open[(int64_t)pair * parts + part] = through;
         }
-        sum[1 - from][tid] = s;
-        open[1 - from][tid] = o;
-        from = 1 - from;
-        __syncthreads();
+        return;
     }
-    double end = 0.0;
+    // what comes from behind this wave
+    double c = 0.0;
     if (a.state_dot)
-        for (int s = 0; s < a.q_slices; ++s) end += (double)a.state_dot[(int64_t)s * n_pairs + pair];
-    double c = end;
-    if (tid + 1 < kThreads) c = sum[from][tid + 1] + (open[from][tid + 1] ? end : 0.0);
+        for (int s = 0; s < a.q_slices; ++s) c += (double)a.state_dot[(int64_t)s * n_pairs + pair];
+    for (int i = parts - 1; i > part; --i) {
+        const int64_t at = (int64_t)pair * parts + i;
+        c = a.part_sums[at] + (a.part_open[at] ? c : 0.0);
+    }
+    for (int i = kThreads / 64 - 1; i > w; --i) c = wave_sums[i] + (wave_open[i] ? c : 0.0);
+    // ... and behind this thread
+    const double s1 = __shfl_down(sum, 1, 64);
+    const int o1 = __shfl_down(open, 1, 64);
+    if (lane < 63) c = s1 + (o1 ? c : 0.0);
     double total = 0.0;
-    for (int t = t1 - 1; t >= t0; --t) {
-        const float gate = gate_at(t);
-        c += x_at(t);
-        double d = c / (double)gate;
-        if (!(gate > wiped)) c = d = 0.0;
+#pragma unroll
+    for (int i = kRun - 1; i >= 0; --i) {
+        const int t = t0 + i;
+        if (t >= a.T) continue;
+        c += x[i];
+        double d = c / (double)gate[i];
+        if (!(gate[i] > kWiped)) c = d = 0.0;
         if (!a.gate_per_head) a.dgate[((int64_t)b * a.T + t) * a.Hkv + h] = (float)d;
         total += d;
     }
     if (a.gate_per_head) {
+#pragma unroll
+        for (int off = 32; off > 0; off /= 2) total += __shfl_xor(total, off, 64);
         __syncthreads();
-        sum[0][tid] = total;
+        if (lane == 0) wave_sums[w] = total;
         __syncthreads();
-        for (int off = kThreads / 2; off > 0; off /= 2) {
-            if (tid < off) sum[0][tid] += sum[0][tid + off];
-            __syncthreads();
+        if (tid == 0) {
+            double all = 0.0;
+            for (int i = 0; i < kThreads / 64; ++i) all += wave_sums[i];
+            a.per_part[(int64_t)pair * parts + part] = all;
         }
-        if (tid == 0) a.per_pair[pair] = sum[0][0];
     }
 }
 
@@ -86,8 +118,10 @@ __global__ __launch_bounds__(64) void linear_gate_heads_kernel(LinearGateArgs a)
 {
     const int h = blockIdx.x * 64 + threadIdx.x;
     if (h >= a.Hkv) return;
+    const int parts = (a.T + kPart - 1) / kPart;
     double x = 0.0;
-    for (int b = 0; b < a.B; ++b) x += a.per_pair[(int64_t)b * a.Hkv + h];
+    for (int b = 0; b < a.B; ++b)
+        for (int i = 0; i < parts; ++i) x += a.per_part[((int64_t)b * a.Hkv + h) * parts + i];
     a.dgate[h] = (float)x;
 }
 
@@ -104,10 +138,27 @@ __global__ __launch_bounds__(256) void linear_state_sum_kernel(const float *per_
 
 }  // namespace
 
-hipError_t launch_linear_gate(const LinearGateArgs &a, hipStream_t stream)
+size_t linear_gate_workspace_bytes(int64_t pairs, int T)
 {
-    hipLaunchKernelGGL(linear_gate_kernel, dim3(a.B * a.Hkv), dim3(kThreads), 0, stream, a);
-    hipError_t e = hipGetLastError();
+    const int64_t parts = ((int64_t)T + kPart - 1) / kPart;
+    return (size_t)(pairs * parts) * (2 * sizeof(double) + sizeof(int));
+}
+
+hipError_t launch_linear_gate(const LinearGateArgs &a0, void *workspace, hipStream_t stream)
+{
+    LinearGateArgs a = a0;
+    const int64_t pairs = (int64_t)a.B * a.Hkv, parts = ((int64_t)a.T + kPart - 1) / kPart;
+    if (pairs * parts > 0x7fffffff) return hipErrorInvalidValue;
+    a.part_sums = (double *)workspace;
+    a.per_part = a.part_sums + pairs * parts;
+    a.part_open = (int *)(a.per_part + pairs * parts);
+    hipError_t e;
+    if (parts > 1) {
+        hipLaunchKernelGGL(linear_gate_kernel<true>, dim3((unsigned)(pairs * parts)), dim3(kThreads), 0, stream, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(linear_gate_kernel<false>, dim3((unsigned)(pairs * parts)), dim3(kThreads), 0, stream, a);
+    e = hipGetLastError();
     if (e != hipSuccess || !a.gate_per_head) return e;
     hipLaunchKernelGGL(linear_gate_heads_kernel, dim3((a.Hkv + 63) / 64), dim3(64), 0, stream, a);
     return hipGetLastError();

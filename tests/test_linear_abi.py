@@ -231,7 +231,7 @@ for device in (0, 1):
             raised[c["mangled"], c["device"]] = c["value"]
         elif c["kind"] == "launch":
             device, seen = int(seen >= half), seen + 1
-            assert 0 < c["grid"] <= 0x7fffffff and c["block"] <= 512 and c["lds"] <= 160 << 10
+            assert 0 < c["grid"] <= 0x7fffffff and c["block"] <= 1024 and c["lds"] <= 160 << 10
             if c["lds"] > 64 << 10:
                 assert raised.get((c["mangled"], device), 0) >= c["lds"], (c["kernel"], device)
     for name in ("linear_walk_kernel", "linear_scan_kernel", "linear_gate_kernel", "linear_decode_kernel", "linear_shared_kernel"):
