@@ -14,19 +14,20 @@ namespace {
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 // ---- decode ----------------------------------------------------------------------------------------------------------
-// A row of the state (one v-feature) lies across LPR lanes, four k-features on each; a thread holds NR rows, a workgroup
-// (256 / LPR) NR of them. The state crosses memory once, whatever the number of tokens. Rows of q, k, v and gates come through LDS, as
-// many tokens at a time as fit, so that their latency is paid once and beside the state's.
+// A row of the state (one v-feature) lies across LPR lanes, 4 J k-features on each (runs of four, 4 LPR apart); a thread holds NR
+// rows, a workgroup (256 / LPR) NR of them. Few lanes to a row: a token costs each of its G heads a sum over them. The state
+// crosses memory once, whatever the number of tokens. Rows of q, k, v and gates come through LDS, as many tokens at a time as
+// fit, so that their latency is paid once and beside the state's.
 constexpr int kDecodeQueries = 32;                 // q rows of a pass through LDS, or those of one token in parts of as many
 constexpr int kDecodeTokens = 16;                  // tokens of a pass at most
 
-template <bool BF16, int LPR, int NR>
+template <bool BF16, int LPR, int J, int NR>
 __global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a, int tokens)
 {
     typedef std::conditional_t<BF16, IOBF16, IOF32> IO;
     typedef typename IO::type elem_t;
     constexpr int RP = 256 / LPR;                  // rows a workgroup covers at once
-    constexpr int DKP = 4 * LPR;                   // k-features with padding
+    constexpr int DKP = 4 * LPR * J;               // k-features with padding
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const int queries = a.G < kDecodeQueries ? a.G : kDecodeQueries;       // heads of a token in LDS at once
     float *sk = lds, *sv = sk + tokens * DKP, *sg = sv + tokens * RP * NR, *sq = sg + kDecodeTokens;
@@ -35,77 +36,89 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a, 
     const int row_first = (int)(blockIdx.x % blocks) * RP * NR;
     const int tid = threadIdx.x, row0 = row_first + tid / LPR;
     const int b = (int)(pair / a.Hkv), h = (int)(pair % a.Hkv);
-    const int l = tid % LPR, col = 4 * l;
-    const bool col_in = col < a.dk;
+    const int l = tid % LPR;
+    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
     const float *S0 = a.S_in + ((int64_t)(b / a.share) * a.Hkv + h) * a.dv * a.dk;
-    f32x4 S[NR];
+    f32x4 S[NR][J];
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-        const int row = row0 + i * RP;
-        S[i] = col_in && row < a.dv ? *(const f32x4 *)(S0 + (int64_t)row * a.dk + col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
+    for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int row = row0 + i * RP, col = 4 * (l + LPR * j);
+            S[i][j] = col < a.dk && row < a.dv ? *(const f32x4 *)(S0 + (int64_t)row * a.dk + col) : zero;
+        }
     auto row_of = [&](const RowTensor &x, int t, int head) { return (const elem_t *)x.p + b * x.sb + t * x.st + head * x.sh; };
-    // q rows of `heads` heads from `head0` on of tokens t0 .. t0 + count - 1
-    auto load_q = [&](int t0, int count, int head0, int heads) {
-        for (int i = tid / LPR; i < count * heads; i += RP)
-            *(f32x4 *)(sq + i * DKP + col) = col_in ? IO::load4(row_of(a.q, t0 + i / heads, h * a.G + head0 + i % heads), col)
-                                                    : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // `count` rows of q or k, the i-th given by where(i), into LDS
+    auto load_rows = [&](float *to, int count, auto where) {
+        for (int i = tid; i < count * (DKP / 4); i += 256) {
+            const int col = 4 * (i % (DKP / 4));
+            *(f32x4 *)(to + 4 * i) = col < a.dk ? IO::load4(where(i / (DKP / 4)), col) : zero;
+        }
     };
     for (int t0 = 0; t0 < a.T; t0 += tokens) {
         const int count = a.T - t0 < tokens ? a.T - t0 : tokens;
         if (t0 > 0) __syncthreads();
-        for (int i = tid / LPR; i < count; i += RP)
-            *(f32x4 *)(sk + i * DKP + col) = col_in ? IO::load4(row_of(a.k, t0 + i, h), col) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        load_rows(sk, count, [&](int i) { return row_of(a.k, t0 + i, h); });
+        load_rows(sq, count * queries, [&](int i) { return row_of(a.q, t0 + i / queries, h * a.G + i % queries); });
         for (int i = tid; i < count * RP * NR; i += 256) {
             const int row = row_first + i % (RP * NR);
             sv[i] = row < a.dv ? IO::load(row_of(a.v, t0 + i / (RP * NR), h), row) : 0.0f;
         }
         if (tid < count) sg[tid] = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + t0 + tid) * a.Hkv + h];
-        load_q(t0, count, 0, queries);
         __syncthreads();
         for (int t = 0; t < count; ++t) {
             const float gate = sg[t];
-            const f32x4 k4 = *(const f32x4 *)(sk + t * DKP + col);
+            float x[NR];
 #pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                const float x = sv[t * RP * NR + i * RP + tid / LPR];
+            for (int i = 0; i < NR; ++i) x[i] = sv[t * RP * NR + i * RP + tid / LPR];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S[i][e] = gate * S[i][e] + x * k4[e];
+            for (int j = 0; j < J; ++j) {
+                const f32x4 k4 = *(const f32x4 *)(sk + t * DKP + 4 * (l + LPR * j));
+#pragma unroll
+                for (int i = 0; i < NR; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) S[i][j][e] = gate * S[i][j][e] + x[i] * k4[e];
             }
+            elem_t *y = const_cast<elem_t *>(row_of(a.y, t0 + t, h * a.G)) + row0;
             for (int head0 = 0; head0 < a.G; head0 += queries) {
                 const int heads = a.G - head0 < queries ? a.G - head0 : queries;
-                if (head0 > 0 || (a.G > queries && t > 0)) {               // (more heads than LDS has room for: part by part)
+                if (head0 > 0) {                   // (more heads than LDS has room for: one token a pass, part by part)
                     __syncthreads();
-                    load_q(t0 + t, 1, head0, heads);
+                    load_rows(sq, heads, [&](int i) { return row_of(a.q, t0 + t, h * a.G + head0 + i); });
                     __syncthreads();
                 }
-                const float *q = sq + (a.G > queries ? 0 : t * queries) * DKP + col;
+                const float *q = sq + t * queries * DKP + 4 * l;
                 for (int s = 0; s < heads; ++s) {
-                    const f32x4 q4 = *(const f32x4 *)(q + s * DKP);
-                    float mine = 0.0f;                     // lane i of the LPR: row i (i < NR), lanes of other NR the same again
+                    float p[NR];
+#pragma unroll
+                    for (int i = 0; i < NR; ++i) p[i] = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        const f32x4 q4 = *(const f32x4 *)(q + s * DKP + 4 * LPR * j);
+#pragma unroll
+                        for (int i = 0; i < NR; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) p[i] += S[i][j][e] * q4[e];
+                    }
+                    float mine = 0.0f;             // lane i of a row's lanes: row i of the thread's
 #pragma unroll
                     for (int i = 0; i < NR; ++i) {
-                        const float p = sum_over_lanes<LPR>((S[i][0] * q4[0] + S[i][1] * q4[1]) + (S[i][2] * q4[2] + S[i][3] * q4[3]));
-                        if (LPR >= NR) mine = l == i ? p : mine;
-                        else if (l == i % LPR) {
-                            const int row = row0 + i * RP;
-                            if (row < a.dv) IO::store1(const_cast<elem_t *>(row_of(a.y, t0 + t, h * a.G + head0 + s)), row, p);
-                        }
+                        const float all = sum_over_lanes<LPR>(p[i]);
+                        mine = l == i ? all : mine;
                     }
-                    if (LPR >= NR && l < NR) {
-                        const int row = row0 + l * RP;
-                        if (row < a.dv) IO::store1(const_cast<elem_t *>(row_of(a.y, t0 + t, h * a.G + head0 + s)), row, mine);
-                    }
+                    if (l < NR && row0 + l * RP < a.dv) IO::store1(y + (head0 + s) * a.y.sh, l * RP, mine);
                 }
             }
         }
     }
     float *S1 = a.S_out + pair * a.dv * a.dk;
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-        const int row = row0 + i * RP;
-        if (col_in && row < a.dv) *(f32x4 *)(S1 + (int64_t)row * a.dk + col) = S[i];
-    }
+    for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int row = row0 + i * RP, col = 4 * (l + LPR * j);
+            if (col < a.dk && row < a.dv) *(f32x4 *)(S1 + (int64_t)row * a.dk + col) = S[i][j];
+        }
 }
 
 // ---- shared ----------------------------------------------------------------------------------------------------------
@@ -326,48 +339,54 @@ int pow2_at_least(int x)
     return p;
 }
 
-template <bool BF16, int LPR, int NR>
-hipError_t launch_decode_kernel(const LinearDecodeArgs &a, int64_t blocks, hipStream_t stream)
+template <bool BF16, int LPR, int J, int NR>
+hipError_t launch_decode_kernel(const LinearDecodeArgs &a, hipStream_t stream)
 {
+    constexpr int ROWS = 256 / LPR * NR;           // of a workgroup
+    const int64_t blocks = (int64_t)a.B * a.Hkv * ((a.dv + ROWS - 1) / ROWS);
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     // tokens of a pass through LDS: as many as all of whose q rows have room
     int tokens = a.G >= kDecodeQueries ? 1 : kDecodeQueries / a.G;
     tokens = tokens < kDecodeTokens ? tokens : kDecodeTokens;
     tokens = tokens < a.T ? tokens : a.T;
     const int queries = a.G < kDecodeQueries ? tokens * a.G : kDecodeQueries;
-    const size_t lds = ((size_t)(tokens + queries) * 4 * LPR + tokens * (256 / LPR) * NR + kDecodeTokens) * sizeof(float);
-    hipLaunchKernelGGL((linear_decode_kernel<BF16, LPR, NR>), dim3((unsigned)blocks), dim3(256), lds, stream, a, tokens);
+    const size_t lds = ((size_t)(tokens + queries) * 4 * LPR * J + tokens * ROWS + kDecodeTokens) * sizeof(float);
+    hipLaunchKernelGGL((linear_decode_kernel<BF16, LPR, J, NR>), dim3((unsigned)blocks), dim3(256), lds, stream, a, tokens);
     return hipGetLastError();
 }
 
-template <bool BF16, int LPR>
-hipError_t launch_decode_rows(const LinearDecodeArgs &a, hipStream_t stream)
+template <bool BF16, int DK>
+hipError_t launch_decode_dk(const LinearDecodeArgs &a, hipStream_t stream)
 {
-    constexpr int RP = 256 / LPR;
     const int64_t pairs = (int64_t)a.B * a.Hkv;
-    // as many rows to a thread as leave four workgroups to a CU
-    const auto blocks = [&](int nr) { return pairs * ((a.dv + RP * nr - 1) / (RP * nr)); };
-    if (blocks(8) >= 1024) return launch_decode_kernel<BF16, LPR, 8>(a, blocks(8), stream);
-    if (blocks(4) >= 1024) return launch_decode_kernel<BF16, LPR, 4>(a, blocks(4), stream);
-    return launch_decode_kernel<BF16, LPR, 1>(a, blocks(1), stream);
+    const auto fills = [&](int rows) { return pairs * ((a.dv + rows - 1) / rows) >= 1024; };   // four workgroups to a CU
+    // One or two query heads to a state: a row lies across as many lanes as it has runs, in one stretch of memory, and a thread takes
+    // eight rows where enough workgroups remain (8192 states of d 128, one token: 187 us against 193, 16 states: 4.2 us against
+    // 4.8). More heads: fewer lanes (384 states, 4 tokens of 4 heads: 17.0 us against 22.2). The number of tokens has no part in
+    // this: several tokens in a call give the same bits as one after the other.
+    if (a.G <= 2)
+        return fills(8 * 256 / (DK / 4)) ? launch_decode_kernel<BF16, DK / 4, 1, (DK < 32 ? DK / 4 : 8)>(a, stream)
+                                         : launch_decode_kernel<BF16, DK / 4, 1, 1>(a, stream);
+    constexpr int LPR = DK <= 16 ? 4 : DK <= 128 ? 8 : 16, J = DK / 4 / LPR;
+    return fills(2 * 256 / LPR) ? launch_decode_kernel<BF16, LPR, J, 2>(a, stream) : launch_decode_kernel<BF16, LPR, J, 1>(a, stream);
 }
 
 template <bool BF16>
 hipError_t launch_decode(const LinearDecodeArgs &a, hipStream_t stream)
 {
-    switch (pow2_at_least(a.dk / 4)) {
-    case 4: return launch_decode_rows<BF16, 4>(a, stream);
-    case 8: return launch_decode_rows<BF16, 8>(a, stream);
-    case 16: return launch_decode_rows<BF16, 16>(a, stream);
-    case 32: return launch_decode_rows<BF16, 32>(a, stream);
-    default: return launch_decode_rows<BF16, 64>(a, stream);
-    }
+    if (a.dk <= 16) return launch_decode_dk<BF16, 16>(a, stream);
+    if (a.dk <= 32) return launch_decode_dk<BF16, 32>(a, stream);
+    if (a.dk <= 64) return launch_decode_dk<BF16, 64>(a, stream);
+    if (a.dk <= 128) return launch_decode_dk<BF16, 128>(a, stream);
+    return launch_decode_dk<BF16, 256>(a, stream);
 }
 
 template <bool BF16, int LR>
 hipError_t launch_shared(const LinearSharedArgs &a, hipStream_t stream)
 {
     const int64_t cols = (int64_t)a.share * a.G, groups = (int64_t)(a.B / a.share) * a.Hkv;
-    // two workgroups to a CU, with fewer columns to each where there are not so many
+    // two workgroups to a CU, with fewer columns to each where there are not so many (four: 75 us instead of 63 for 64 samples of 4
+    // prefixes, 32 heads)
     int ncol = kSharedCols;
     while (ncol > 1 && groups * ((cols + ncol - 1) / ncol) < 512) ncol /= 2;
     const int64_t blocks = groups * ((cols + ncol - 1) / ncol);
