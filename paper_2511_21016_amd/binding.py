@@ -514,119 +514,47 @@ def _linear_params(q, k, v, gate, out=None, states=None, lead=None, cache_tokens
                               (0, 0, 0) if out is None else _row_strides(out, "out"))
 
 
-class _OnDevice:
-    """Makes the tensors' device the current one, where it is another: a launch goes to the current device."""
+class _LinearPlan:
+    """What a call needs to know of its tensors' shapes, strides, types and device: the checks are passed, these the parameters."""
+    __slots__ = ("params", "forward_bytes", "backward_bytes")
 
-    def __init__(self, index):
-        import torch
-        self.guard = None if torch.cuda.current_device() == index else torch.cuda.device(index)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+    def __init__(self, params):
+        self.params = params
+        self.forward_bytes = self.backward_bytes = None
 
 
-def _workspace_for(nbytes, workspace, device, name_the_error):
-    import torch
-    if nbytes == 0:
-        _check(name_the_error())                   # let the library say what is wrong with the parameters
-    if workspace is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if workspace.get_device() != device.index or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous and on the tensors' device")
-    return workspace
+_linear_plans = {}          # what _linear_plan was asked for -> _LinearPlan
 
 
-def linear_workspace(q, k, v, gate, *, backward=False, walk_chunks=0):
-    """A workspace for calls of gka_linear_forward (or gka_linear_backward) with tensors of these sizes, for programs that
-    keep one. Two calls that may run at the same time (other streams, other graphs) need one each."""
-    import torch
-    load_library()
-    _stream_of(q)
-    params = _linear_params(q, k, v, gate, lead=4, walk_chunks=walk_chunks)
-    if backward:
-        nbytes = linear_backward_workspace_bytes(params)
-    else:
-        nbytes = linear_forward_workspace_bytes(params)
-    if nbytes == 0:
-        _check(linear_forward_raw(params, None, None, None, None, None))
-    return torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+def _linear_plan(call, option, q, k, v, gate, rows, S, T=None, kc=None, vc=None, gc=None, n=None):
+    """The plan of a call with these tensors, checked once for each set of shapes, strides, types and devices (a decode step of
+    one sequence lasts as long as the Python that enqueues it). Nothing in it depends on where the tensors lie."""
+    key = (call, option, *[x if x is None else (x.shape, x.stride(), x.dtype, x.get_device())
+                           for x in (q, k, v, gate, rows, S, T, kc, vc, gc, n)])
+    plan = _linear_plans.get(key)
+    if plan is None:
+        if len(_linear_plans) >= 1024:
+            _linear_plans.clear()
+        plan = _linear_plans[key] = _LinearPlan(_LINEAR_CHECKS[call](option, q, k, v, gate, rows, S, T, kc, vc, gc, n))
+    return plan
 
 
-def gka_linear_forward(q, k, v, gate, *, S_init=None, return_state=False, workspace=None, out=None, S_final=None,
-                       walk_chunks=0):
-    """gka_linear_forward on torch CUDA tensors: q [B,T,H,d_k], k [B,T,H_kv,d_k], v [B,T,H_kv,d_v] (float32 or bfloat16, any
-    strides with contiguous features), gate [B,T,H_kv] float32 or [H_kv] (one decay for each head); S_init: states
-    [B,H_kv,d_v,d_k] float32 to continue from, or [B/F,..]: each is shared by F consecutive sequences. Returns o [B,T,H,d_v],
-    with return_state (or a buffer S_final for them) also the states after the last token."""
-    import torch
-    load_library()
-    stream = _stream_of(q)
-    o = torch.empty((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device) if out is None else out
-    params = _linear_params(q, k, v, gate, o, [("S_init", S_init, True), ("S_final", S_final, False)], 4, walk_chunks=walk_chunks)
-    workspace = _workspace_for(linear_forward_workspace_bytes(params), workspace, q.device,
-                               lambda: linear_forward_raw(params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(o)))
-    if S_final is None and return_state:
-        S_final = torch.empty((q.shape[0], *v.shape[2:], q.shape[-1]), dtype=torch.float32, device=q.device)
-    with _OnDevice(q.get_device()):
-        _check(linear_forward_raw(params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(o), _ptr(S_init), _ptr(S_final),
-                                  _ptr(workspace), workspace.numel() * workspace.element_size(), stream))
-    return o if S_final is None else (o, S_final)
+def _check_walk(walk_chunks, q, k, v, gate, o, S_init, S_final, *_):
+    return _linear_params(q, k, v, gate, o, [("S_init", S_init, True), ("S_final", S_final, False)], 4, walk_chunks=walk_chunks)
 
 
-def gka_linear_backward(q, k, v, gate, dy, *, S_init=None, dS_final=None, workspace=None, walk_chunks=0):
-    """gka_linear_backward on torch CUDA tensors: the arguments of gka_linear_forward, dy [B,T,H,d_v] like its output and
-    dS_final [B,H_kv,d_v,d_k] the gradient at its final states. Returns a dict: dq, dk, dv in the tensors' dtype (packed),
-    dgate float32 like gate and, with S_init, dS_init like it (summed over the sequences that share a state)."""
-    import torch
-    load_library()
-    stream = _stream_of(q)
-    params = _linear_params(q, k, v, gate, dy, [("S_init", S_init, True), ("dS_final", dS_final, False)], 4, walk_chunks=walk_chunks)
-    out = {"dq": torch.empty(q.shape, dtype=q.dtype, device=q.device), "dk": torch.empty(k.shape, dtype=k.dtype, device=k.device),
-           "dv": torch.empty(v.shape, dtype=v.dtype, device=v.device), "dgate": torch.empty_like(gate)}
-    if S_init is not None:
-        out["dS_init"] = torch.empty_like(S_init)
-    grads = [_ptr(out[n]) for n in ("dq", "dk", "dv", "dgate")]
-    workspace = _workspace_for(linear_backward_workspace_bytes(params), workspace, q.device,
-                               lambda: linear_backward_raw(params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(dy), *grads))
-    with _OnDevice(q.get_device()):
-        _check(linear_backward_raw(params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(dy), *grads, _ptr(S_init), _ptr(dS_final),
-                                   _ptr(out.get("dS_init")), _ptr(workspace), workspace.numel() * workspace.element_size(), stream))
-    return out
+def _check_backward(walk_chunks, q, k, v, gate, dy, S_init, dS_final, *_):
+    return _linear_params(q, k, v, gate, dy, [("S_init", S_init, True), ("dS_final", dS_final, False)], 4, walk_chunks=walk_chunks)
 
 
-def gka_linear_decode(S, q, k, v, gate, *, S_out=None, out=None):
-    """gka_linear_decode on torch CUDA tensors: states S [B,H_kv,d_v,d_k] float32, updated in place unless S_out is given (S may
-    then be [B/F,..], each state shared by F consecutive sequences); one token q [B,H,d_k], k, v, gate [B,H_kv], or T of
-    them with a token dimension behind the batch as in gka_linear_forward; gate [H_kv]: one decay for each head."""
-    import torch
-    load_library()
-    stream = _stream_of(q)
+def _check_decode(in_place, q, k, v, gate, o, S, S_out, *_):
     if q.dim() not in (3, 4):
         raise ValueError("q: expected [B, H, d_k] or [B, T, H, d_k]")
-    o = torch.empty((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device) if out is None else out
-    target = S if S_out is None else S_out
-    params = _linear_params(q, k, v, gate, o, [("S", S, S_out is not None), ("S_out", target, False)])
-    with _OnDevice(q.get_device()):
-        _check(linear_decode_raw(params, _ptr(S), _ptr(target), _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(o), stream))
-    return o
+    return _linear_params(q, k, v, gate, o, [("S", S, not in_place), ("S_out", S_out, False)])
 
 
-def gka_linear_decode_shared(S_prefix, q, k, v, gate, k_cache, v_cache, gate_cache, lengths, *, out=None):
-    """gka_linear_decode_shared on torch CUDA tensors: one token q [B,H,d_k], k [B,H_kv,d_k], v [B,H_kv,d_v], gate [B,H_kv] (or
-    [H_kv], then gate_cache is None) of B sequences, B/P consecutive ones of which continue each of the P prefixes whose
-    states S_prefix [P,H_kv,d_v,d_k] are; k_cache [B,N,H_kv,d_k], v_cache [B,N,H_kv,d_v], gate_cache [B,N,H_kv]: the
-    tokens behind the prefix, lengths [B] int32 how many of them there are; row lengths[b] is filled by the call. Sequences
-    with lengths outside 0 .. N - 1 take no part: their rows of the caches and of `out` stay as they are (without `out`:
-    unspecified)."""
+def _check_shared(_, q, k, v, gate, o, S_prefix, T, k_cache, v_cache, gate_cache, lengths):
     import torch
-    load_library()
-    stream = _stream_of(q)
-    o = torch.empty((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device) if out is None else out
     if k_cache.dim() != 4:
         raise ValueError("k_cache: expected [B, N, H_kv, d_k]")
     B, N = q.shape[0], k_cache.shape[1]
@@ -640,7 +568,125 @@ def gka_linear_decode_shared(S_prefix, q, k, v, gate, k_cache, v_cache, gate_cac
             raise ValueError(f"{name}: expected contiguous {(B, N, *rows)} {dtype} on the tensors' device")
     if lengths.shape != (B,) or lengths.dtype != torch.int32 or not lengths.is_contiguous() or lengths.get_device() != q.get_device():
         raise ValueError(f"lengths: expected contiguous {(B,)} int32 on the tensors' device")
-    with _OnDevice(q.get_device()):
-        _check(linear_decode_shared_raw(params, _ptr(S_prefix), _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(k_cache), _ptr(v_cache),
-                                        _ptr(gate_cache), _ptr(lengths), _ptr(o), stream))
+    return params
+
+
+_LINEAR_CHECKS = {"forward": _check_walk, "backward": _check_backward, "decode": _check_decode, "shared": _check_shared}
+
+
+def _on_device(index, call, *args):
+    """call(*args) with the tensors' device as the current one, where a launch goes."""
+    import torch
+    if torch.cuda.current_device() == index:
+        return call(*args)
+    with torch.cuda.device(index):
+        return call(*args)
+
+
+def _workspace_for(nbytes, workspace, device):
+    import torch
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if workspace.get_device() != device.index or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the tensors' device")
+    return workspace
+
+
+def _workspace_bytes(plan, backward):
+    nbytes = plan.backward_bytes if backward else plan.forward_bytes
+    if nbytes is None:
+        nbytes = (linear_backward_workspace_bytes if backward else linear_forward_workspace_bytes)(plan.params)
+        if nbytes == 0:                            # let the library say what is wrong with the parameters
+            _check(linear_forward_raw(plan.params, None, None, None, None, None))
+        if backward:
+            plan.backward_bytes = nbytes
+        else:
+            plan.forward_bytes = nbytes
+    return nbytes
+
+
+def linear_workspace(q, k, v, gate, *, backward=False, walk_chunks=0):
+    """A workspace for calls of gka_linear_forward (or gka_linear_backward) with tensors of these sizes, for programs that
+    keep one. Two calls that may run at the same time (other streams, other graphs) need one each."""
+    import torch
+    load_library()
+    _stream_of(q)
+    plan = _linear_plan("forward", walk_chunks, q, k, v, gate, None, None)
+    return torch.empty(_workspace_bytes(plan, backward), dtype=torch.uint8, device=q.device)
+
+
+def gka_linear_forward(q, k, v, gate, *, S_init=None, return_state=False, workspace=None, out=None, S_final=None,
+                       walk_chunks=0):
+    """gka_linear_forward on torch CUDA tensors: q [B,T,H,d_k], k [B,T,H_kv,d_k], v [B,T,H_kv,d_v] (float32 or bfloat16, any
+    strides with contiguous features), gate [B,T,H_kv] float32 or [H_kv] (one decay for each head); S_init: states
+    [B,H_kv,d_v,d_k] float32 to continue from, or [B/F,..]: each is shared by F consecutive sequences. Returns o [B,T,H,d_v],
+    with return_state (or a buffer S_final for them) also the states after the last token."""
+    load_library()
+    stream = _stream_of(q)
+    o = out
+    if o is None:
+        import torch
+        o = torch.empty((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device)
+    plan = _linear_plan("forward", walk_chunks, q, k, v, gate, o, S_init, S_final)
+    workspace = _workspace_for(_workspace_bytes(plan, False), workspace, q.device)
+    if S_final is None and return_state:
+        import torch
+        S_final = torch.empty((q.shape[0], *v.shape[2:], q.shape[-1]), dtype=torch.float32, device=q.device)
+    _check(_on_device(q.get_device(), linear_forward_raw, plan.params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(o), _ptr(S_init),
+                      _ptr(S_final), _ptr(workspace), workspace.numel() * workspace.element_size(), stream))
+    return o if S_final is None else (o, S_final)
+
+
+def gka_linear_backward(q, k, v, gate, dy, *, S_init=None, dS_final=None, workspace=None, walk_chunks=0):
+    """gka_linear_backward on torch CUDA tensors: the arguments of gka_linear_forward, dy [B,T,H,d_v] like its output and
+    dS_final [B,H_kv,d_v,d_k] the gradient at its final states. Returns a dict: dq, dk, dv in the tensors' dtype (packed),
+    dgate float32 like gate and, with S_init, dS_init like it (summed over the sequences that share a state)."""
+    import torch
+    load_library()
+    stream = _stream_of(q)
+    plan = _linear_plan("backward", walk_chunks, q, k, v, gate, dy, S_init, dS_final)
+    out = {"dq": torch.empty(q.shape, dtype=q.dtype, device=q.device), "dk": torch.empty(k.shape, dtype=k.dtype, device=k.device),
+           "dv": torch.empty(v.shape, dtype=v.dtype, device=v.device), "dgate": torch.empty_like(gate)}
+    if S_init is not None:
+        out["dS_init"] = torch.empty_like(S_init)
+    workspace = _workspace_for(_workspace_bytes(plan, True), workspace, q.device)
+    _check(_on_device(q.get_device(), linear_backward_raw, plan.params, _ptr(q), _ptr(k), _ptr(v), _ptr(gate), _ptr(dy),
+                      *[_ptr(out[n]) for n in ("dq", "dk", "dv", "dgate")], _ptr(S_init), _ptr(dS_final), _ptr(out.get("dS_init")),
+                      _ptr(workspace), workspace.numel() * workspace.element_size(), stream))
+    return out
+
+
+def gka_linear_decode(S, q, k, v, gate, *, S_out=None, out=None):
+    """gka_linear_decode on torch CUDA tensors: states S [B,H_kv,d_v,d_k] float32, updated in place unless S_out is given (S may
+    then be [B/F,..], each state shared by F consecutive sequences); one token q [B,H,d_k], k, v, gate [B,H_kv], or T of
+    them with a token dimension behind the batch as in gka_linear_forward; gate [H_kv]: one decay for each head."""
+    load_library()
+    stream = _stream_of(q)
+    o = out
+    if o is None:
+        import torch
+        o = torch.empty((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device)
+    target = S if S_out is None else S_out
+    plan = _linear_plan("decode", target is S, q, k, v, gate, o, S, target)
+    _check(_on_device(q.get_device(), linear_decode_raw, plan.params, _ptr(S), _ptr(target), _ptr(q), _ptr(k), _ptr(v), _ptr(gate),
+                      _ptr(o), stream))
+    return o
+
+
+def gka_linear_decode_shared(S_prefix, q, k, v, gate, k_cache, v_cache, gate_cache, lengths, *, out=None):
+    """gka_linear_decode_shared on torch CUDA tensors: one token q [B,H,d_k], k [B,H_kv,d_k], v [B,H_kv,d_v], gate [B,H_kv] (or
+    [H_kv], then gate_cache is None) of B sequences, B/P consecutive ones of which continue each of the P prefixes whose
+    states S_prefix [P,H_kv,d_v,d_k] are; k_cache [B,N,H_kv,d_k], v_cache [B,N,H_kv,d_v], gate_cache [B,N,H_kv]: the
+    tokens behind the prefix, lengths [B] int32 how many of them there are; row lengths[b] is filled by the call. Sequences
+    with lengths outside 0 .. N - 1 take no part: their rows of the caches and of `out` stay as they are (without `out`:
+    unspecified)."""
+    load_library()
+    stream = _stream_of(q)
+    o = out
+    if o is None:
+        import torch
+        o = torch.empty((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device)
+    plan = _linear_plan("shared", None, q, k, v, gate, o, S_prefix, None, k_cache, v_cache, gate_cache, lengths)
+    _check(_on_device(q.get_device(), linear_decode_shared_raw, plan.params, _ptr(S_prefix), _ptr(q), _ptr(k), _ptr(v), _ptr(gate),
+                      _ptr(k_cache), _ptr(v_cache), _ptr(gate_cache), _ptr(lengths), _ptr(o), stream))
     return o
