@@ -76,6 +76,14 @@ struct SwizzledTile16 {
     static __device__ __forceinline__ int further(int offset, int pieces) { return offset ^ pieces * 16; }
 };
 
+// Place of a piece of row `row` + `pass` ROWS: a fixed distance on where ROWS is a multiple of 16, after which the swizzle repeats.
+template <class T, int ROWS>
+__device__ __forceinline__ int row_of_pass(int row, int piece, int pass)
+{
+    if constexpr (ROWS % 16 == 0) return T::at(row, piece) + pass * ROWS * T::ROW;
+    else return T::at(row + pass * ROWS, piece);
+}
+
 // The value again, as one that the compiler does not know: what is computed from it inside a loop is not kept in registers across
 // it (some thirty offsets into the swizzled tiles, one XOR each, spilled otherwise).
 __device__ __forceinline__ int anew(int x)
@@ -255,6 +263,27 @@ __device__ __forceinline__ int chunk_offset(const RowTensor &x, int row, int col
     return exists ? (reverse ? -row : row) * pitch + col * ES : (int)0x80000000;
 }
 
+// use(0), .., use(N - 1), each after load(i) into one of two buffers, the next load issued before: LDS reads travel while the products
+// of the ones before run. (Left to itself the compiler puts every read right in front of its product and waits for it.)
+template <int I, int N, class Buffer, class Load, class Use>
+__device__ __forceinline__ void in_flight_step(Buffer (&buffer)[2], Load load, Use use)
+{
+    if constexpr (I < N) {
+        if constexpr (I + 1 < N) load(std::integral_constant<int, I + 1>{}, buffer[(I + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        use(std::integral_constant<int, I>{}, buffer[I & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        in_flight_step<I + 1, N>(buffer, load, use);
+    }
+}
+template <int N, class Buffer, class Load, class Use>
+__device__ __forceinline__ void in_flight(Load load, Use use)
+{
+    Buffer buffer[2];
+    load(std::integral_constant<int, 0>{}, buffer[0]);
+    in_flight_step<0, N>(buffer, load, use);
+}
+
 enum Group { kOne, kQueries, kSources };           // n_q = n_src = 1; several queries; several sources of a token
 
 // Waves on a SIMD that a kernel's registers are limited for: two workgroups of a CU's LDS, one with 256 k-features.
@@ -273,15 +302,16 @@ void linear_walk_kernel(LinearWalkArgs a)
     constexpr bool BF16 = M::BF16;
     constexpr int C = SH::C, TB = SH::TB, SB = SH::SB, NT = SH::NT, NJ = SH::NJ, KB = SH::KB, E = SH::E, ES = SH::ES, PK = SH::PK,
                   PV = SH::PV, STEPS = M::STEPS, VEC = M::VEC;
+    constexpr bool ROOMY = walk_waves(DK, NW) == 2;
+    constexpr int LOOKAHEAD = ROOMY ? 4 : GROUP == kSources ? 1 : 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char *sK = smem, *sV = smem + SH::k_bytes;
     float *tables = (float *)(sV + SH::v_bytes);   // [2][5][64]: log2 decay (two floats), weight in the state, zeta of a token; zeta_C
     unsigned char *sQ = (unsigned char *)tables + SH::tables, *sP = sQ + SH::q_bytes;
 
     const int tid = threadIdx.x;
-    const int lane = tid & 63;
+    const int lane0 = tid & 63, lane = lane0;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 15, kg = lane >> 4;
     const int n_pairs = a.B * a.Hkv;
     const int pair = blockIdx.x % n_pairs;
     const int slice = blockIdx.x / n_pairs % a.slices;
@@ -299,50 +329,61 @@ void linear_walk_kernel(LinearWalkArgs a)
         u32x4_t q[SUMMARY ? 1 : PK], k[PK], v[PV];
     };
     constexpr int KROW = DK / E, VROW = 16 * NW / E;          // pieces of a row
-    const int krow = tid / KROW, kpiece = tid % KROW;         // (a thread's pieces all lie in one column)
-    const int vrow = tid / VROW, vpiece = tid % VROW;
-    const int q_off = chunk_offset<ES>(a.q, krow, E * kpiece, E * kpiece < a.dk, a.reverse);
-    const int k_off = chunk_offset<ES>(a.k, krow, E * kpiece, E * kpiece < a.dk, a.reverse);
-    const int v_off = chunk_offset<ES>(a.v, vrow, v0 + E * vpiece, v0 + E * vpiece < a.dv, a.reverse);
-    auto fetch_rows = [&](auto &to, const RowTensor &x, int head, int tau0, int offset, int rows_per) {
-        const ChunkRows r = chunk_rows<C, ES>(x, b, head, tau0, a.T, a.reverse);
+    // (a thread's pieces all lie in one column)
+    const int q_off = chunk_offset<ES>(a.q, tid / KROW, E * (tid % KROW), E * (tid % KROW) < a.dk, a.reverse);
+    const int k_off = chunk_offset<ES>(a.k, tid / KROW, E * (tid % KROW), E * (tid % KROW) < a.dk, a.reverse);
+    const int v_off = chunk_offset<ES>(a.v, tid / VROW, v0 + E * (tid % VROW), v0 + E * (tid % VROW) < a.dv, a.reverse);
+    // (chunks behind the segment: an empty buffer, zeros without a read. Every path writes the registers, so that they are not
+    // held from where they are staged to where the next rows are asked for.)
+    auto fetch_rows = [&](auto &to, const RowTensor &x, int head, int tau0, bool exists, int offset, int rows_per) {
+        const ChunkRows r = chunk_rows<C, ES>(x, b, head, exists ? tau0 : 0, exists ? a.T : 0, a.reverse);
         const int step = chunk_offset<ES>(x, rows_per, 0, true, a.reverse);
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(to) / 16); ++i)
             to[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r.rows, offset + (r.top + i * step), 0, 0));
     };
+    auto no_rows = [&](auto &to) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(to) / 16); ++i) to[i] = u32x4_t{0, 0, 0, 0};
+    };
     auto fetch = [&](Rows &f, int c, int s) {
-        if constexpr (!SUMMARY)
-            if (GROUP == kQueries || s == 0) fetch_rows(f.q, a.q, GROUP == kQueries ? h * steps + s : h, c * C, q_off, NT / KROW);
+        const bool exists = c < chunk_end;
+        if constexpr (!SUMMARY) {
+            if (GROUP == kQueries || s == 0) fetch_rows(f.q, a.q, GROUP == kQueries ? h * steps + s : h, c * C, exists, q_off, NT / KROW);
+            else no_rows(f.q);
+        }
         if (GROUP == kSources || s == 0) {
             const int head = GROUP == kSources ? h * steps + s : h;
-            fetch_rows(f.k, a.k, head, c * C, k_off, NT / KROW);
-            fetch_rows(f.v, a.v, head, c * C, v_off, NT / VROW);
+            fetch_rows(f.k, a.k, head, c * C, exists, k_off, NT / KROW);
+            fetch_rows(f.v, a.v, head, c * C, exists, v_off, NT / VROW);
+        } else {
+            no_rows(f.k);
+            no_rows(f.v);
         }
     };
     auto stage = [&](const Rows &f, int s) {
+        const int thread = anew(tid);
+        const int krow = thread / KROW, kpiece = thread % KROW;
         if constexpr (!SUMMARY)
             if (GROUP == kQueries || s == 0) {
+                const int j = kpiece & 3, to = kpiece & ~3, half = 8 * (j >> 1);
 #pragma unroll
                 for (int i = 0; i < PK; ++i) {
-                    const int row = krow + i * (NT / KROW);
                     if constexpr (BF16) {
-                        const int j = kpiece & 3, to = kpiece & ~3, half = 8 * (j >> 1);
-                        *(u32x2_t *)(sQ + QT::at(row, to + (2 * j & 3)) + half) = u32x2_t{f.q[i][0], f.q[i][1]};
-                        *(u32x2_t *)(sQ + QT::at(row, to + (2 * j & 3) + 1) + half) = u32x2_t{f.q[i][2], f.q[i][3]};
+                        *(u32x2_t *)(sQ + row_of_pass<QT, NT / KROW>(krow, to + (2 * j & 3), i) + half) = u32x2_t{f.q[i][0], f.q[i][1]};
+                        *(u32x2_t *)(sQ + row_of_pass<QT, NT / KROW>(krow, to + (2 * j & 3) + 1, i) + half) = u32x2_t{f.q[i][2], f.q[i][3]};
                     } else {
-                        *(u32x4_t *)(sQ + QT::at(row, kpiece)) = f.q[i];
+                        *(u32x4_t *)(sQ + row_of_pass<QT, NT / KROW>(krow, kpiece, i)) = f.q[i];
                     }
                 }
             }
         if (GROUP == kSources || s == 0) {
 #pragma unroll
-            for (int i = 0; i < PK; ++i) *(u32x4_t *)(sK + KT::at(krow + i * (NT / KROW), kpiece)) = f.k[i];
+            for (int i = 0; i < PK; ++i) *(u32x4_t *)(sK + row_of_pass<KT, NT / KROW>(krow, kpiece, i)) = f.k[i];
 #pragma unroll
-            for (int i = 0; i < PV; ++i) *(u32x4_t *)(sV + VT::at(vrow + i * (NT / VROW), vpiece)) = f.v[i];
+            for (int i = 0; i < PV; ++i) *(u32x4_t *)(sV + row_of_pass<VT, NT / VROW>(thread / VROW, thread % VROW, i)) = f.v[i];
         }
     };
-
     const int q_lane = q_place<QT>(lane), k_lane = k_place<M, KT>(lane), kt_lane = col_place<M, KT>(lane);
     const int v_lane = VT::further(col_place<M, VT>(lane), w * (16 * ES / 16));
 
@@ -415,8 +456,11 @@ void linear_walk_kernel(LinearWalkArgs a)
         for (int s = 0; s < steps; ++s) {
             lds_barrier();                         // the tiles of the step before have been read
             stage(rows, s);
-            if (s + 1 < steps) fetch(rows, c, s + 1);
-            else if (c + 1 < chunk_end) fetch(rows, c + 1, 0);
+            auto fetch_next = [&] {
+                const bool more = GROUP != kOne && s + 1 < steps;
+                fetch(rows, more ? c : c + 1, more ? s + 1 : 0);
+            };
+            if (SUMMARY || ROOMY) fetch_next();
             lds_barrier();                         // (no wait for the rows in flight)
             __builtin_amdgcn_sched_barrier(0);
             if (w == NW - 1 && s == 0 && c + 1 < chunk_end) {
@@ -428,18 +472,30 @@ void linear_walk_kernel(LinearWalkArgs a)
                 // ---- masked products M[t, s] (k_s . q_t): a unit is a block of 16 tokens and 32 keys, left as operand fragments
                 const int k_at = anew(k_lane);
                 int q_at = anew(q_lane);
+                const int lane = anew(lane0), n = lane & 15, kg = lane >> 4;
                 for (int unit = w; unit < SH::UNITS; unit += NW) {
                     const int tb = unit < 2 ? unit : 1 + unit / 2, sb = unit < 2 ? 0 : unit & 1;
-                    f32x4 x[2];
+                    f32x4 x[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+                    constexpr int PB = !BF16 ? 1 : KB < LOOKAHEAD ? KB : LOOKAHEAD;        // 32-blocks of features in flight
+                    frag qf[PB][STEPS], kf[2][PB][STEPS];
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        x[half] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                        if (2 * sb + half > tb) continue;
+                    for (int k0 = 0; k0 < KB; k0 += PB) {
 #pragma unroll
-                        for (int kb = 0; kb < KB; ++kb)
+                        for (int kb = 0; kb < PB; ++kb)
 #pragma unroll
-                            for (int st = 0; st < STEPS; ++st)
-                                x[half] = M::mma(k_frag<M, KT>(sK, k_at, 32 * sb + 16 * half, kb, st), q_frag<M, QT>(sQ, q_at, 16 * tb, kb, st), x[half]);
+                            for (int st = 0; st < STEPS; ++st) {
+                                qf[kb][st] = q_frag<M, QT>(sQ, q_at, 16 * tb, k0 + kb, st);
+                                kf[0][kb][st] = k_frag<M, KT>(sK, k_at, 32 * sb, k0 + kb, st);
+                                kf[1][kb][st] = k_frag<M, KT>(sK, k_at, 32 * sb + 16, k0 + kb, st);
+                            }
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int kb = 0; kb < PB; ++kb)
+#pragma unroll
+                            for (int st = 0; st < STEPS; ++st) {
+                                x[0] = M::mma(kf[0][kb][st], qf[kb][st], x[0]);
+                                x[1] = M::mma(kf[1][kb][st], qf[kb][st], x[1]);
+                            }
                     }
                     // register r: key 32 sb + 16 half + 4 kg + r, token 16 tb + n
                     const float hi = sHi[16 * tb + n], lo = sLo[16 * tb + n];
@@ -450,7 +506,8 @@ void linear_walk_kernel(LinearWalkArgs a)
                         const f32x4 h4 = *(const f32x4 *)(sHi + s0), l4 = *(const f32x4 *)(sLo + s0);
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            m[4 * half + r] = s0 + r <= 16 * tb + n ? x[half][r] * __builtin_amdgcn_exp2f((hi - h4[r]) + (lo - l4[r])) : 0.0f;
+                            // (behind the token: 2^-1000 = 0; the select before the exp2 leaves no branch)
+                            m[4 * half + r] = x[half][r] * __builtin_amdgcn_exp2f(s0 + r <= 16 * tb + n ? (hi - h4[r]) + (lo - l4[r]) : -1000.0f);
                     }
 #pragma unroll
                     for (int st = 0; st < STEPS; ++st) {
@@ -466,22 +523,27 @@ void linear_walk_kernel(LinearWalkArgs a)
                 q_at = anew(q_at);
                 if (GROUP == kQueries || s == 0) {
 #pragma unroll
-                    for (int tb = 0; tb < TB; ++tb) y[tb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
                     for (int kb = 0; kb < KB; ++kb) {
-                        const float x[8] = {acc[2 * kb][0], acc[2 * kb][1], acc[2 * kb][2], acc[2 * kb][3],
-                                            acc[2 * kb + 1][0], acc[2 * kb + 1][1], acc[2 * kb + 1][2], acc[2 * kb + 1][3]};
+                        // (the reads travel while the state is cut)
+                        frag qf[TB][STEPS];
+#pragma unroll
+                        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                            for (int st = 0; st < STEPS; ++st) qf[tb][st] = q_frag<M, QT>(sQ, q_at, 16 * tb, kb, st);
+                        __builtin_amdgcn_sched_barrier(0);
+                        const f32x4 lo = acc[2 * kb], hi = acc[2 * kb + 1];
+                        const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 #pragma unroll
                         for (int st = 0; st < STEPS; ++st) {
                             frag f[PIECES];
                             cut<M, PIECES>(x + VEC * st, f);
 #pragma unroll
-                            for (int tb = 0; tb < TB; ++tb) {
-                                const frag qf = q_frag<M, QT>(sQ, q_at, 16 * tb, kb, st);
+                            for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-                                for (int i = 0; i < PIECES; ++i) y[tb] = M::mma(f[i], qf, y[tb]);
-                            }
+                                for (int tb = 0; tb < TB; ++tb)
+                                    y[tb] = M::mma(f[i], qf[tb][st], kb == 0 && st == 0 && i == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : y[tb]);
                         }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
 #pragma unroll
                     for (int tb = 0; tb < TB; ++tb) {
@@ -490,10 +552,7 @@ void linear_walk_kernel(LinearWalkArgs a)
                         for (int r = 0; r < 4; ++r) y[tb][r] *= zeta;
                     }
                 }
-                lds_barrier();                     // the masked products are there
-                __builtin_amdgcn_sched_barrier(0);
             }
-
             frag vt[SB][STEPS];                    // v, features on the lanes, contraction over the tokens
 #pragma unroll
             for (int sb = 0; sb < SB; ++sb)
@@ -501,18 +560,32 @@ void linear_walk_kernel(LinearWalkArgs a)
                 for (int st = 0; st < STEPS; ++st) vt[sb][st] = col_frag<M, VT>(sV, v_lane, 0, sb, st);
 
             if constexpr (!SUMMARY) {
+                // (asked for only now where registers are few: half a chunk ahead, with none of them held through the products before)
+                if (!ROOMY) fetch_next();
+                lds_barrier();                     // the masked products are there
+                __builtin_amdgcn_sched_barrier(0);
                 // ---- + sum_s v_s M[t, s] (k_s . q_t)
+                const int products = anew(lane0);
+                struct Products {
+                    frag f[!BF16 ? 8 : ROOMY ? 3 : LOOKAHEAD];
+                };
+                constexpr int BATCH = sizeof(Products) / sizeof(frag);
+                in_flight<PIECES * SH::UNITS * STEPS / BATCH, Products>(
+                    [&](auto i, Products &p) {
 #pragma unroll
-                for (int unit = 0; unit < SH::UNITS; ++unit) {
-                    const int tb = unit < 2 ? unit : 1 + unit / 2, sb = unit < 2 ? 0 : unit & 1;
+                        for (int e = 0; e < BATCH; ++e) p.f[e] = ((const frag *)sP)[(i * BATCH + e) * 64 + products];
+                    },
+                    [&](auto i, const Products &p) {
 #pragma unroll
-                    for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-                        for (int i = 0; i < PIECES; ++i)
-                            y[tb] = M::mma(vt[sb][st], ((const frag *)sP)[((i * SH::UNITS + unit) * STEPS + st) * 64 + lane], y[tb]);
-                }
+                        for (int e = 0; e < BATCH; ++e) {
+                            const int at = i * BATCH + e, st = at % STEPS, unit = at / STEPS % SH::UNITS;
+                            const int tb = unit < 2 ? unit : 1 + unit / 2, sb = unit < 2 ? 0 : unit & 1;
+                            y[tb] = M::mma(vt[sb][st], p.f[e], y[tb]);
+                        }
+                    });
                 // ---- out: register r holds feature v0 + 16 w + 4 kg + r of token 16 tb + n
                 if (GROUP == kQueries || s + 1 == steps) {
+                    const int lane = anew(lane0), n = lane & 15, kg = lane >> 4;
                     const int head = GROUP == kQueries ? h * steps + s : h;
                     const int col = v0 + 16 * w + 4 * kg;
                     const bool in = v0 + 16 * w < a.dv;
@@ -578,27 +651,41 @@ void linear_walk_kernel(LinearWalkArgs a)
                 for (int j = 0; j < NJ; ++j) acc[j] *= zeta_C;
             }
             if (GROUP == kSources || s + 1 == steps) {
-                const int kt_at = anew(kt_lane);
+                const int kt_at = anew(kt_lane), kg = anew(lane0) >> 4;
+                // BATCH tiles of the state at a time, the steps of the contraction over the tokens on the outside
+                constexpr int BATCH = !BF16 ? (NJ < 8 ? NJ : 8) : LOOKAHEAD, PARTS = NJ / BATCH;
+                struct Keys {
+                    frag f[BATCH];
+                };
+                frag f[VW];
+                in_flight<SB * STEPS * PARTS, Keys>(
+                    [&](auto i, Keys &k) {
+                        constexpr int part = i % PARTS, st = i / PARTS % STEPS, sb = i / PARTS / STEPS;
 #pragma unroll
-                for (int sb = 0; sb < SB; ++sb) {
-                    const f32x4 w0 = *(const f32x4 *)(sW + 32 * sb + 4 * kg), w1 = *(const f32x4 *)(sW + 32 * sb + 16 + 4 * kg);
-                    const float wt[8] = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
+                        for (int e = 0; e < BATCH; ++e) k.f[e] = col_frag<M, KT>(sK, kt_at, part * BATCH + e, sb, st);
+                    },
+                    [&](auto i, const Keys &k) {
+                        constexpr int part = i % PARTS, st = i / PARTS % STEPS, sb = i / PARTS / STEPS;
+                        if constexpr (part == 0) {
+                            float x[VEC];
+                            M::unpack(vt[sb][st], x);
+                            if constexpr (BF16) {
+                                const f32x4 w0 = *(const f32x4 *)(sW + 32 * sb + 4 * kg), w1 = *(const f32x4 *)(sW + 32 * sb + 16 + 4 * kg);
 #pragma unroll
-                    for (int st = 0; st < STEPS; ++st) {
-                        float x[VEC];
-                        M::unpack(vt[sb][st], x);
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) x[e] *= wt[VEC * st + e];
-                        frag f[VW];
-                        cut<M, VW>(x, f);
-#pragma unroll
-                        for (int j = 0; j < NJ; ++j) {
-                            const frag kt = col_frag<M, KT>(sK, kt_at, j, sb, st);
-#pragma unroll
-                            for (int i = 0; i < VW; ++i) acc[j] = M::mma(kt, f[i], acc[j]);
+                                for (int e = 0; e < 4; ++e) {
+                                    x[e] *= w0[e];
+                                    x[4 + e] *= w1[e];
+                                }
+                            } else {
+                                x[0] *= sW[32 * sb + 16 * (st >> 2) + 4 * kg + (st & 3)];
+                            }
+                            cut<M, VW>(x, f);
                         }
-                    }
-                }
+#pragma unroll
+                        for (int n_piece = 0; n_piece < VW; ++n_piece)
+#pragma unroll
+                            for (int e = 0; e < BATCH; ++e) acc[part * BATCH + e] = M::mma(k.f[e], f[n_piece], acc[part * BATCH + e]);
+                    });
             }
         }
     }
