@@ -10,6 +10,8 @@ SOURCES = ["gka_api.hip", "gka_state_pass.hip", "gka_chunk_solve.hip", "gka_solv
            "gka_fused.hip", "gka_decode.hip", "gka_backward.hip", "gka_readout.hip", "gka_reverse.hip",
            "gka_sketch.hip", "gka_small_dim.hip", "gka_linear_api.hip", "gka_linear_bf16_64.hip", "gka_linear_bf16_128.hip",
            "gka_linear_bf16_256.hip", "gka_linear_f32_64.hip", "gka_linear_f32_128.hip", "gka_linear_f32_256.hip",
+           "gka_linear_backward_bf16_64.hip", "gka_linear_backward_bf16_128.hip", "gka_linear_backward_bf16_256.hip",
+           "gka_linear_backward_f32_64.hip", "gka_linear_backward_f32_128.hip", "gka_linear_backward_f32_256.hip",
            "gka_linear_gradient.hip", "gka_linear_decode.hip"]
 # Host code of the boundary: argument validation, launch plans, workspace carving.
 API_SOURCES = ["gka_api.hip", "gka_linear_api.hip"]

@@ -443,4 +443,18 @@ __device__ __forceinline__ float sum_over_lanes(float x)
 // base 2): cumulative sums of these, and exp2 of their differences.
 __device__ __forceinline__ float log2_gate(float gamma) { return fmaxf(log2f(gamma), kMinLog2Gate); }
 
+// log2(gamma) in float64, with the same floor. Close to 1, where float32's logarithm is off by some 2^-24 of 1 and so by far more of
+// itself, from the series of log(1 - x), whose terms from the third on are small enough for float32 (relative error 2^-31): a
+// decay of 1 - 2^-9 for a thousand tokens would be off by 2^-14 otherwise.
+__device__ __forceinline__ double log2_gate_f64(float gamma)
+{
+    const double x = 1.0 - (double)gamma;
+    const float f = (float)x;
+    float s = 1.0f / 12.0f;
+#pragma unroll
+    for (int n = 11; n >= 3; --n) s = s * f + 1.0f / n;
+    const double near_one = -1.4426950408889634 * (x + x * x * (0.5 + (double)(f * s)));
+    return fabsf(f) <= 0.125f ? near_one : (double)log2_gate(gamma);
+}
+
 }  // namespace gka

@@ -43,6 +43,7 @@ struct LinearWalkArgs {
     float *seg_states;            // [B, H_kv, slices, n_segs, slice, DK] in the kernel's order: what each segment adds, then the
                                   // state that it starts from
     float *seg_decay;             // [B, H_kv, n_segs]
+    int seg_turned[3];            // not 0: seg_states are those of the walk with transposed states: its waves, tiles a wave, slices
 };
 
 // Tokens of a chunk, features of a slice and padded dk of the kernels for these sizes; floats of a segment's state.
@@ -51,13 +52,29 @@ struct LinearShape {
     int64_t state_floats;
 };
 LinearShape linear_shape(bool bf16, int dk, int dv);
-hipError_t launch_linear_walk(const LinearWalkArgs &a, bool bf16, hipStream_t stream);
-hipError_t launch_linear_walk_bf16_64(const LinearWalkArgs &a, hipStream_t stream);      // (padded_dk)
-hipError_t launch_linear_walk_bf16_128(const LinearWalkArgs &a, hipStream_t stream);
-hipError_t launch_linear_walk_bf16_256(const LinearWalkArgs &a, hipStream_t stream);
-hipError_t launch_linear_walk_f32_64(const LinearWalkArgs &a, hipStream_t stream);
-hipError_t launch_linear_walk_f32_128(const LinearWalkArgs &a, hipStream_t stream);
-hipError_t launch_linear_walk_f32_256(const LinearWalkArgs &a, hipStream_t stream);
+// The forward pass, and the three walks of the backward pass, with the summaries of their segments. dk's and dv's have the same
+// segments; those of dv need seg_states and seg_decay of dk's.
+hipError_t launch_linear_forward(const LinearWalkArgs &a, bool bf16, hipStream_t stream);
+hipError_t launch_linear_backward(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool bf16, hipStream_t stream);
+// ... by type and padded_dk
+hipError_t launch_linear_forward_bf16_64(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_values_bf16_64(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_backward_bf16_64(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream);
+hipError_t launch_linear_forward_bf16_128(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_values_bf16_128(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_backward_bf16_128(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream);
+hipError_t launch_linear_forward_bf16_256(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_values_bf16_256(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_backward_bf16_256(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream);
+hipError_t launch_linear_forward_f32_64(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_values_f32_64(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_backward_f32_64(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream);
+hipError_t launch_linear_forward_f32_128(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_values_f32_128(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_backward_f32_128(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream);
+hipError_t launch_linear_forward_f32_256(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_values_f32_256(const LinearWalkArgs &a, hipStream_t stream);
+hipError_t launch_linear_backward_f32_256(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream);
 
 // dgate_t = ([state_dot] + sum_{s >= t} (q . dq - k . dk)) / gate_t, and the sum of gradients at shared initial states.
 struct LinearGateArgs {

@@ -88,11 +88,12 @@ struct WalkPlan {
     size_t state_bytes, decay_bytes;   // of the segments' states and decays in the workspace
 };
 
-gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv, WalkPlan *w)
+// slices: of dv, of the walk whose workgroups the segments are counted for (0: of this one).
+gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv, int slices, WalkPlan *w)
 {
     w->shape = gka::linear_shape(s.bf16, dk, dv);
     const int64_t chunks = ((int64_t)p->T + w->shape.chunk - 1) / w->shape.chunk;
-    const int64_t walks = s.pairs * w->shape.slices;
+    const int64_t walks = s.pairs * (slices > 0 ? slices : w->shape.slices);
     int64_t segs = 1;
     if (p->walk_chunks > 0) {
         segs = (chunks + p->walk_chunks - 1) / p->walk_chunks;
@@ -104,9 +105,9 @@ gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv,
         w->seg_chunks = (int)((chunks + segs - 1) / segs);
     }
     w->n_segs = (int)((chunks + w->seg_chunks - 1) / w->seg_chunks);
-    const int64_t states = walks * w->n_segs;
-    // (the scan runs state_floats / 1024 workgroups for each state of a walk)
-    if (states > 0x7fffffff || walks * (w->shape.state_floats / 1024) > 0x7fffffff) return GKA_ERR_SHAPE;
+    const int64_t states = s.pairs * w->shape.slices * w->n_segs;
+    // (the scan runs state_floats / 1024 workgroups for each state of a walk; three walks are one launch)
+    if (states > 0x7fffffff / 4 || s.pairs * w->shape.slices * (w->shape.state_floats / 1024) > 0x7fffffff) return GKA_ERR_SHAPE;
     w->state_bytes = w->n_segs > 1 ? align_up((size_t)states * w->shape.state_floats * sizeof(float), 256) : 0;
     w->decay_bytes = w->n_segs > 1 ? align_up((size_t)s.pairs * w->n_segs * sizeof(float), 256) : 0;
     return GKA_OK;
@@ -132,19 +133,20 @@ gka::LinearWalkArgs walk_args(const gka_linear_params *p, const Sizes &s, const 
 struct BackwardPlan {
     Sizes s;
     WalkPlan q, k, v;                  // the walks of dq, dk, dv
-    size_t off_q_dot, off_k_dot, off_state_dot, off_gate, off_states, total;
+    size_t off_q, off_k, off_q_dot, off_k_dot, off_state_dot, off_gate, off_states, total;
 };
 
 gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
 {
     gka_status e = check(p, Call::kWalk, &b->s);
     if (e != GKA_OK) return e;
-    if ((e = plan_walk(p, b->s, p->d_v, p->d_k, &b->q)) != GKA_OK) return e;
+    // (the walks of dk and dv have their segments in common)
+    if ((e = plan_walk(p, b->s, p->d_v, p->d_k, 0, &b->q)) != GKA_OK) return e;
     b->k = b->q;
-    if ((e = plan_walk(p, b->s, p->d_k, p->d_v, &b->v)) != GKA_OK) return e;
+    if ((e = plan_walk(p, b->s, p->d_k, p->d_v, b->q.shape.slices, &b->v)) != GKA_OK) return e;
     size_t off = 0;
-    for (const WalkPlan *w : {&b->q, &b->v})
-        if (off < w->state_bytes + w->decay_bytes) off = w->state_bytes + w->decay_bytes;
+    b->off_q = off; off += b->q.state_bytes + b->q.decay_bytes;
+    b->off_k = off; off += b->k.state_bytes + b->k.decay_bytes;
     const size_t tokens = (size_t)b->s.pairs * p->T;
     b->off_q_dot = off; off += align_up(b->q.shape.slices * tokens * b->s.G * sizeof(float), 256);
     b->off_k_dot = off; off += align_up(b->k.shape.slices * tokens * sizeof(float), 256);
@@ -172,12 +174,36 @@ LinearShape linear_shape(bool bf16, int dk, int dv)
     return s;
 }
 
-hipError_t launch_linear_walk(const LinearWalkArgs &a, bool bf16, hipStream_t stream)
+hipError_t launch_linear_forward(const LinearWalkArgs &a, bool bf16, hipStream_t stream)
 {
     switch (linear_shape(bf16, a.dk, a.dv).padded_dk) {
-    case 64: return bf16 ? launch_linear_walk_bf16_64(a, stream) : launch_linear_walk_f32_64(a, stream);
-    case 128: return bf16 ? launch_linear_walk_bf16_128(a, stream) : launch_linear_walk_f32_128(a, stream);
-    default: return bf16 ? launch_linear_walk_bf16_256(a, stream) : launch_linear_walk_f32_256(a, stream);
+    case 64: return bf16 ? launch_linear_forward_bf16_64(a, stream) : launch_linear_forward_f32_64(a, stream);
+    case 128: return bf16 ? launch_linear_forward_bf16_128(a, stream) : launch_linear_forward_f32_128(a, stream);
+    default: return bf16 ? launch_linear_forward_bf16_256(a, stream) : launch_linear_forward_f32_256(a, stream);
+    }
+}
+
+hipError_t launch_linear_backward(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool bf16, hipStream_t stream)
+{
+    const LinearShape of_dk = linear_shape(bf16, dk.dk, dk.dv), of_dv = linear_shape(bf16, dv.dk, dv.dv);
+    LinearWalkArgs v = dv;
+    v.seg_states = dk.seg_states;
+    v.seg_decay = dk.seg_decay;
+    v.seg_turned[0] = of_dk.slice / 16;
+    v.seg_turned[1] = of_dk.padded_dk / 16;
+    v.seg_turned[2] = of_dk.slices;
+    const bool alike = of_dk.padded_dk == of_dv.padded_dk && of_dk.slice == of_dv.slice && of_dk.slices == of_dv.slices;
+    hipError_t e;
+    switch (of_dk.padded_dk) {
+    case 64: e = bf16 ? launch_linear_backward_bf16_64(dq, dk, v, alike, stream) : launch_linear_backward_f32_64(dq, dk, v, alike, stream); break;
+    case 128: e = bf16 ? launch_linear_backward_bf16_128(dq, dk, v, alike, stream) : launch_linear_backward_f32_128(dq, dk, v, alike, stream); break;
+    default: e = bf16 ? launch_linear_backward_bf16_256(dq, dk, v, alike, stream) : launch_linear_backward_f32_256(dq, dk, v, alike, stream);
+    }
+    if (e != hipSuccess || alike) return e;
+    switch (of_dv.padded_dk) {
+    case 64: return bf16 ? launch_linear_values_bf16_64(v, stream) : launch_linear_values_f32_64(v, stream);
+    case 128: return bf16 ? launch_linear_values_bf16_128(v, stream) : launch_linear_values_f32_128(v, stream);
+    default: return bf16 ? launch_linear_values_bf16_256(v, stream) : launch_linear_values_f32_256(v, stream);
     }
 }
 
@@ -189,7 +215,7 @@ size_t gka_linear_forward_workspace_bytes(const gka_linear_params *p)
 {
     Sizes s;
     WalkPlan w;
-    if (check(p, Call::kWalk, &s) != GKA_OK || plan_walk(p, s, p->d_k, p->d_v, &w) != GKA_OK) return 0;
+    if (check(p, Call::kWalk, &s) != GKA_OK || plan_walk(p, s, p->d_k, p->d_v, 0, &w) != GKA_OK) return 0;
     const size_t bytes = w.state_bytes + w.decay_bytes;
     return bytes > 0 ? bytes : 256;
 }
@@ -201,7 +227,7 @@ gka_status gka_linear_forward(const gka_linear_params *p, const void *q, const v
     WalkPlan w;
     gka_status e = check(p, Call::kWalk, &s);
     if (e != GKA_OK) return e;
-    if ((e = plan_walk(p, s, p->d_k, p->d_v, &w)) != GKA_OK) return e;
+    if ((e = plan_walk(p, s, p->d_k, p->d_v, 0, &w)) != GKA_OK) return e;
     if (!q || !k || !v || !gate || !o) return GKA_ERR_NULL;
     if (misaligned({q, k, v, o, S_init, S_final})) return GKA_ERR_SHAPE;
     if (S_final && S_final == S_init && s.share > 1) return GKA_ERR_SHAPE;   // (states that other sequences still read)
@@ -212,7 +238,7 @@ gka_status gka_linear_forward(const gka_linear_params *p, const void *q, const v
     a.n_q = s.G;
     a.init = S_init; a.share = s.share;
     a.final = S_final;
-    return gka::launch_linear_walk(a, s.bf16, (hipStream_t)hip_stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
+    return gka::launch_linear_forward(a, s.bf16, (hipStream_t)hip_stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
 }
 
 size_t gka_linear_backward_workspace_bytes(const gka_linear_params *p)
@@ -240,40 +266,35 @@ gka_status gka_linear_backward(const gka_linear_params *p, const void *q, const 
     (void)row_strides(none, p, p->T, p->H, p->d_k, &packed_q);
     (void)row_strides(none, p, p->T, p->H_kv, p->d_k, &packed_k);
     (void)row_strides(none, p, p->T, p->H_kv, p->d_v, &packed_v);
-    {   // dq_t = S_t^T dy_t
-        gka::LinearWalkArgs a = walk_args(p, s, b.q, gate, p->d_v, p->d_k, ws);
-        a.q = at(dy, s.o); a.k = at(v, s.v); a.v = at(k, s.k); a.y = at(dq, packed_q);
-        a.n_q = s.G;
-        a.init = S_init; a.share = s.share; a.transposed = 1;
-        a.dot_with = at(q, s.q); a.dot_out = q_dot;
-        if (dS_final) {
-            a.state_dot_with = dS_final;
-            a.state_dot_out = state_dot;
-        }
-        if (gka::launch_linear_walk(a, s.bf16, stream) != hipSuccess) return GKA_ERR_LAUNCH;
+    // dq_t = S_t^T dy_t
+    gka::LinearWalkArgs wq = walk_args(p, s, b.q, gate, p->d_v, p->d_k, ws + b.off_q);
+    wq.q = at(dy, s.o); wq.k = at(v, s.v); wq.v = at(k, s.k); wq.y = at(dq, packed_q);
+    wq.n_q = s.G;
+    wq.init = S_init; wq.share = s.share; wq.transposed = 1;
+    wq.dot_with = at(q, s.q); wq.dot_out = q_dot;
+    if (dS_final) {
+        wq.state_dot_with = dS_final;
+        wq.state_dot_out = state_dot;
     }
-    {   // dk_t = dS_t^T v_t, dS_t = sum_g dy_t q_t^T + gate_{t+1} dS_{t+1}
-        gka::LinearWalkArgs a = walk_args(p, s, b.k, gate, p->d_v, p->d_k, ws);
-        a.q = at(v, s.v); a.k = at(dy, s.o); a.v = at(q, s.q); a.y = at(dk, packed_k);
-        a.n_src = s.G;
-        a.reverse = 1;
-        a.init = dS_final; a.transposed = 1;
-        a.dot_with = at(k, s.k); a.dot_out = k_dot;
-        if (gka::launch_linear_walk(a, s.bf16, stream) != hipSuccess) return GKA_ERR_LAUNCH;
-    }
-    {   // dv_t = dS_t k_t
-        gka::LinearWalkArgs a = walk_args(p, s, b.v, gate, p->d_k, p->d_v, ws);
-        a.q = at(k, s.k); a.k = at(q, s.q); a.v = at(dy, s.o); a.y = at(dv, packed_v);
-        a.n_src = s.G;
-        a.reverse = 1;
-        a.init = dS_final;
-        a.final = dS_init && s.share > 1 ? (float *)(ws + b.off_states) : dS_init;
-        a.final_times_gate = 1;
-        if (gka::launch_linear_walk(a, s.bf16, stream) != hipSuccess) return GKA_ERR_LAUNCH;
-        if (dS_init && s.share > 1 &&
-            gka::launch_linear_state_sum(a.final, dS_init, p->B / s.share, s.share, (int64_t)p->H_kv * p->d_k * p->d_v, stream) != hipSuccess)
-            return GKA_ERR_LAUNCH;
-    }
+    // dk_t = dS_t^T v_t, dS_t = sum_g dy_t q_t^T + gate_{t+1} dS_{t+1}
+    gka::LinearWalkArgs wk = walk_args(p, s, b.k, gate, p->d_v, p->d_k, ws + b.off_k);
+    wk.q = at(v, s.v); wk.k = at(dy, s.o); wk.v = at(q, s.q); wk.y = at(dk, packed_k);
+    wk.n_src = s.G;
+    wk.reverse = 1;
+    wk.init = dS_final; wk.transposed = 1;
+    wk.dot_with = at(k, s.k); wk.dot_out = k_dot;
+    // dv_t = dS_t k_t
+    gka::LinearWalkArgs wv = walk_args(p, s, b.v, gate, p->d_k, p->d_v, ws + b.off_k);
+    wv.q = at(k, s.k); wv.k = at(q, s.q); wv.v = at(dy, s.o); wv.y = at(dv, packed_v);
+    wv.n_src = s.G;
+    wv.reverse = 1;
+    wv.init = dS_final;
+    wv.final = dS_init && s.share > 1 ? (float *)(ws + b.off_states) : dS_init;
+    wv.final_times_gate = 1;
+    if (gka::launch_linear_backward(wq, wk, wv, s.bf16, stream) != hipSuccess) return GKA_ERR_LAUNCH;
+    if (dS_init && s.share > 1 &&
+        gka::launch_linear_state_sum(wv.final, dS_init, p->B / s.share, s.share, (int64_t)p->H_kv * p->d_k * p->d_v, stream) != hipSuccess)
+        return GKA_ERR_LAUNCH;
     gka::LinearGateArgs g = {};
     g.q_dq = q_dot; g.k_dk = k_dot; g.state_dot = dS_final ? state_dot : nullptr;
     g.q_slices = b.q.shape.slices; g.k_slices = b.k.shape.slices; g.G = s.G;

@@ -261,7 +261,7 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
             double lg = 0.0;
             if (lane < count) {
                 const float gate = a.gate_per_head || j0 + lane == len ? gate_new : a.gate_cache[cache_row + (int64_t)(j0 + lane) * a.Hkv];
-                lg = (double)log2_gate(gate);
+                lg = log2_gate_f64(gate);
             }
             for (int s0 = 0; s0 < count; s0 += FLY * RP) {
                 piece p[FLY];

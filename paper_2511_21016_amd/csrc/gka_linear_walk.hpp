@@ -198,6 +198,42 @@ __device__ __forceinline__ int64_t seg_state_at(const LinearWalkArgs &a, int64_t
     return ((pair * a.slices + slice) * a.n_segs + seg) * state_floats;
 }
 
+// The segments' states as wave w of a slice reads them: its own tile j (written by the same wave of a summary), or, where they are
+// those of the walk with transposed states (seg_turned: waves, tiles a wave and slices of that walk), the lane's elements of the
+// tile with rows and columns exchanged.
+template <bool TURNED>
+struct SegStates {
+    const float *p;
+    int64_t step;                                  // floats from a segment to the next
+    int row_block, waves, tiles, slices, n_segs;
+    __device__ __forceinline__ SegStates(const LinearWalkArgs &a, int64_t pair, int slice, int w, int lane, int NW, int NJ)
+    {
+        if constexpr (!TURNED) {
+            step = (int64_t)NW * NJ * 256;
+            p = a.seg_states + seg_state_at(a, pair, slice, 0, step) + (w * NJ * 64 + lane) * 4;
+        } else {
+            waves = a.seg_turned[0];
+            tiles = a.seg_turned[1];
+            slices = a.seg_turned[2];
+            n_segs = a.n_segs;
+            step = (int64_t)waves * tiles * 256;
+            row_block = slice * NW + w;            // its 16 v-features are that walk's k-features of this tile
+            p = a.seg_states + pair * slices * n_segs * step + (16 * ((lane & 15) >> 2) + 4 * (lane >> 4)) * 4 + (lane & 3);
+        }
+    }
+    __device__ __forceinline__ f32x4 load(int seg, int j) const
+    {
+        if constexpr (!TURNED) return *(const f32x4 *)(p + seg * step + j * 256);
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int slice = j / waves, w = j % waves;
+        if (row_block >= tiles || slice >= slices) return x;
+        const float *from = p + ((int64_t)slice * n_segs + seg) * step + (w * tiles + row_block) * 256;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = from[4 * r];
+        return x;
+    }
+};
+
 // A caller's state [dv, dk] (or stored [dk, dv]) as a raw buffer: rows and columns of the padding read as zeros, writes to them are
 // dropped. Lane 16 kg + n of the wave whose first v-feature is `row0`: run j is its elements [16 j + 4 kg .. + 3][row0 + n].
 struct StateAt {
@@ -290,9 +326,9 @@ enum Group { kOne, kQueries, kSources };           // n_q = n_src = 1; several q
 constexpr int walk_waves(int dk, int nw) { return nw == 8 && dk <= 128 ? 4 : 2; }
 
 // PIECES: of states and masked products in the readout, VW: of the weighted v (float32 tensors: 1). DOT: dot_out is wanted.
-template <class M, int DK, int NW, int PIECES, int VW, bool DOT, bool SUMMARY, Group GROUP>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(walk_waves(DK, NW), walk_waves(DK, NW))))
-void linear_walk_kernel(LinearWalkArgs a)
+// TURNED: see SegStates.
+template <class M, int DK, int NW, int PIECES, int VW, bool DOT, bool SUMMARY, Group GROUP, bool TURNED = false>
+__device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
 {
     typedef Shape<M, DK, NW> SH;
     typedef typename SH::QT QT;
@@ -313,9 +349,9 @@ void linear_walk_kernel(LinearWalkArgs a)
     const int lane0 = tid & 63, lane = lane0;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n_pairs = a.B * a.Hkv;
-    const int pair = blockIdx.x % n_pairs;
-    const int slice = blockIdx.x / n_pairs % a.slices;
-    const int seg = blockIdx.x / n_pairs / a.slices;
+    const int pair = workgroup % n_pairs;
+    const int slice = workgroup / n_pairs % a.slices;
+    const int seg = workgroup / n_pairs / a.slices;
     const int b = pair / a.Hkv, h = pair % a.Hkv;
     const int n_chunks = (a.T + C - 1) / C;
     const int chunk_begin = seg * a.seg_chunks;
@@ -396,7 +432,7 @@ void linear_walk_kernel(LinearWalkArgs a)
             gate = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + (a.reverse ? a.T - tau : tau)) * a.Hkv + h];
     };
     auto decays = [&](int c) {
-        const double G = wave_inclusive_scan_f64((double)log2_gate(gate)), total = lane63_f64(G);
+        const double G = wave_inclusive_scan_f64(log2_gate_f64(gate)), total = lane63_f64(G);
         const float hi = (float)G, zeta_C = __builtin_amdgcn_exp2f((float)total);
         float *t = tables + (c & 1) * 320 + lane;
         t[0] = hi;
@@ -416,10 +452,10 @@ void linear_walk_kernel(LinearWalkArgs a)
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if constexpr (!SUMMARY) {
-        const float *s = a.seg_states + seg_state_at(a, pair, slice, 0, state_floats) + (w * NJ * 64 + lane) * 4;
+        const SegStates<TURNED> states(a, pair, slice, w, lane, NW, NJ);
         if (a.n_segs > 1 && a.scanned) {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[j] = *(const f32x4 *)(s + seg * state_floats + j * 256);
+            for (int j = 0; j < NJ; ++j) acc[j] = states.load(seg, j);
         } else {
             if (a.init) {
                 const StateAt S(a.init, (int64_t)(b / a.share) * a.Hkv + h, a, v0 + 16 * w, lane);
@@ -430,15 +466,14 @@ void linear_walk_kernel(LinearWalkArgs a)
             f32x4 next[NJ];
             if (seg > 0) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) next[j] = *(const f32x4 *)(s + j * 256);
+                for (int j = 0; j < NJ; ++j) next[j] = states.load(0, j);
             }
             for (int before = 0; before < seg; ++before) {
                 const float decay = a.seg_decay[(int64_t)pair * a.n_segs + before];
-                const int64_t behind = (before + 1 < seg ? before + 1 : before) * state_floats;
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
                     const f32x4 adds = next[j];
-                    next[j] = *(const f32x4 *)(s + behind + j * 256);
+                    next[j] = states.load(before + 1 < seg ? before + 1 : before, j);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[j][r] = decay * acc[j][r] + adds[r];
                 }
@@ -719,11 +754,37 @@ void linear_walk_kernel(LinearWalkArgs a)
         if (a.final) {
             const StateAt S(a.final, pair, a, v0 + 16 * w, lane);
             float scale = 1.0f;
-            if (a.final_times_gate) scale = __builtin_amdgcn_exp2f(log2_gate(a.gate_per_head ? a.gate[h] : a.gate[(int64_t)b * a.T * a.Hkv + h]));
+            if (a.final_times_gate) scale = a.gate_per_head ? a.gate[h] : a.gate[(int64_t)b * a.T * a.Hkv + h];
 #pragma unroll
             for (int j = 0; j < NJ; ++j) S.store(j, acc[j] * scale);
         }
     }
+}
+
+template <class M, int DK, int NW, int PIECES, int VW, bool SUMMARY, Group GROUP, bool TURNED>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(walk_waves(DK, NW), walk_waves(DK, NW))))
+void linear_walk_kernel(LinearWalkArgs a)
+{
+    walk<M, DK, NW, PIECES, VW, false, SUMMARY, GROUP, TURNED>(a, blockIdx.x);
+}
+
+// The walks of the backward pass in one launch, `walks` of them (dq, dk, dv; SUMMARY: dq, dk), groups of eight workgroups of each in
+// turn: workgroups go round the eight XCDs, so that the walks of a pair's segment meet in one L2 and share its rows, and the
+// GPU runs empty once instead of three times.
+struct LinearBackwardArgs {
+    LinearWalkArgs walk[3];
+    int workgroups;                                // of each
+};
+template <class M, int DK, int NW, bool SUMMARY, bool GROUPED, int WALKS>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(walk_waves(DK, NW), walk_waves(DK, NW))))
+void linear_backward_kernel(LinearBackwardArgs a)
+{
+    constexpr int EXACT = M::BF16 ? 3 : 1, PLAIN = M::BF16 ? 2 : 1;
+    const int role = blockIdx.x / 8 % WALKS, workgroup = blockIdx.x / (8 * WALKS) * 8 + blockIdx.x % 8;
+    if (workgroup >= a.workgroups) return;
+    if (role == 0) walk<M, DK, NW, SUMMARY ? 1 : EXACT, EXACT, !SUMMARY, SUMMARY, GROUPED && !SUMMARY ? kQueries : kOne>(a.walk[0], workgroup);
+    else if (role == 1) walk<M, DK, NW, SUMMARY ? 1 : EXACT, EXACT, !SUMMARY, SUMMARY, GROUPED ? kSources : kOne>(a.walk[1], workgroup);
+    else if constexpr (WALKS == 3) walk<M, DK, NW, PLAIN, EXACT, false, false, GROUPED ? kSources : kOne, true>(a.walk[2], workgroup);
 }
 
 // What the segments add -> the states that they start from, in place: a thread carries four floats of a state over the segments.
@@ -751,51 +812,101 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(LinearWalkArgs a)
     }
 }
 
-template <class M, int DK, int NW, int PIECES, int VW, bool DOT, bool SUMMARY, Group GROUP>
-hipError_t launch_kernel(const LinearWalkArgs &a, int workgroups, hipStream_t stream)
+template <class Kernel, class Args>
+hipError_t launch_kernel(Kernel kernel, bool (&raised)[kMaxLdsDevices], int workgroups, int threads, size_t lds, const Args &a, hipStream_t stream)
 {
-    typedef Shape<M, DK, NW> SH;
-    constexpr size_t lds = SH::lds_bytes(PIECES, SUMMARY);
-    static_assert(lds <= (size_t)160 << 10, "LDS of a CU");
-    static bool raised[kMaxLdsDevices] = {};
-    const hipError_t e = raise_lds_limits(raised, {{(const void *)linear_walk_kernel<M, DK, NW, PIECES, VW, DOT, SUMMARY, GROUP>, lds}});
+    const hipError_t e = raise_lds_limits(raised, {{(const void *)kernel, lds}});
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((linear_walk_kernel<M, DK, NW, PIECES, VW, DOT, SUMMARY, GROUP>), dim3(workgroups), dim3(SH::NT), lds, stream, a);
+    hipLaunchKernelGGL(kernel, dim3(workgroups), dim3(threads), lds, stream, a);
     return hipGetLastError();
 }
 
-// VW: pieces of the weighted v
+template <class M, int DK, int NW, int PIECES, int VW, bool SUMMARY, Group GROUP, bool TURNED = false>
+hipError_t launch_one(const LinearWalkArgs &a, hipStream_t stream)
+{
+    typedef Shape<M, DK, NW> SH;
+    static_assert(SH::lds_bytes(3, false) <= (size_t)160 << 10, "LDS of a CU");
+    static bool raised[kMaxLdsDevices] = {};
+    return launch_kernel(linear_walk_kernel<M, DK, NW, PIECES, VW, SUMMARY, GROUP, TURNED>, raised,
+                         a.B * a.Hkv * a.slices * (SUMMARY ? a.n_segs - 1 : a.n_segs), SH::NT, SH::lds_bytes(PIECES, SUMMARY), a, stream);
+}
+
+template <class M, int DK, int NW>
+hipError_t launch_scan(const LinearWalkArgs &a, hipStream_t stream)
+{
+    hipLaunchKernelGGL((linear_scan_kernel<DK, NW>), dim3(a.B * a.Hkv * a.slices * (16 * NW * DK / 1024)), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+// The forward pass. VW: pieces of the weighted v.
 template <class M, int DK, int NW, Group GROUP, int VW>
-hipError_t launch_walk_vw(const LinearWalkArgs &a, hipStream_t stream)
+hipError_t launch_forward_vw(const LinearWalkArgs &a, hipStream_t stream)
 {
-    const int n = a.B * a.Hkv * a.slices;
     if (a.n_segs > 1) {
-        hipError_t e = launch_kernel<M, DK, NW, 1, VW, false, true, GROUP == kSources ? kSources : kOne>(a, n * (a.n_segs - 1), stream);
+        hipError_t e = launch_one<M, DK, NW, 1, VW, true, kOne>(a, stream);
+        if (e == hipSuccess && a.scanned) e = launch_scan<M, DK, NW>(a, stream);
         if (e != hipSuccess) return e;
-        if (a.scanned) {
-            hipLaunchKernelGGL((linear_scan_kernel<DK, NW>), dim3(n * (16 * NW * DK / 1024)), dim3(256), 0, stream, a);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
     }
-    if constexpr (VW != 2)
-        if (a.dot_out) return launch_kernel<M, DK, NW, M::BF16 ? 3 : 1, VW, true, false, GROUP>(a, n * a.n_segs, stream);
-    return launch_kernel<M, DK, NW, M::BF16 ? 2 : 1, VW, false, false, GROUP>(a, n * a.n_segs, stream);
+    return launch_one<M, DK, NW, M::BF16 ? 2 : 1, VW, false, GROUP>(a, stream);
 }
-
 template <class M, int DK, int NW, Group GROUP>
-hipError_t launch_walk(const LinearWalkArgs &a, hipStream_t stream)
+hipError_t launch_forward(const LinearWalkArgs &a, hipStream_t stream)
 {
-    if constexpr (M::BF16) return a.dot_out || a.final ? launch_walk_vw<M, DK, NW, GROUP, 3>(a, stream) : launch_walk_vw<M, DK, NW, GROUP, 2>(a, stream);
-    else return launch_walk_vw<M, DK, NW, GROUP, 1>(a, stream);
+    if constexpr (M::BF16) return a.final ? launch_forward_vw<M, DK, NW, GROUP, 3>(a, stream) : launch_forward_vw<M, DK, NW, GROUP, 2>(a, stream);
+    else return launch_forward_vw<M, DK, NW, GROUP, 1>(a, stream);
 }
-
 template <class M, int DK>
-hipError_t launch_walk_dk(const LinearWalkArgs &a, hipStream_t stream)
+hipError_t launch_forward_dk(const LinearWalkArgs &a, hipStream_t stream)
 {
     const bool narrow = a.dv <= 64;
-    if (a.n_q > 1) return narrow ? launch_walk<M, DK, 4, kQueries>(a, stream) : launch_walk<M, DK, 8, kQueries>(a, stream);
-    if (a.n_src > 1) return narrow ? launch_walk<M, DK, 4, kSources>(a, stream) : launch_walk<M, DK, 8, kSources>(a, stream);
-    return narrow ? launch_walk<M, DK, 4, kOne>(a, stream) : launch_walk<M, DK, 8, kOne>(a, stream);
+    if (a.n_q > 1) return narrow ? launch_forward<M, DK, 4, kQueries>(a, stream) : launch_forward<M, DK, 8, kQueries>(a, stream);
+    return narrow ? launch_forward<M, DK, 4, kOne>(a, stream) : launch_forward<M, DK, 8, kOne>(a, stream);
+}
+
+// The backward pass: dq and dk have states of one shape. dv's, the same as dk's but transposed, start from what dk's segments left;
+// where they are of the same padded shape, the three walks are one launch.
+template <class M, int DK, int NW, bool GROUPED>
+hipError_t launch_backward(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream)
+{
+    typedef Shape<M, DK, NW> SH;
+    constexpr int PIECES = M::BF16 ? 3 : 1;
+    LinearBackwardArgs a = {{dq, dk, dv}, 0};
+    const int pairs = dq.B * dq.Hkv * dq.slices;
+    const auto grid = [&](int walks) { return (a.workgroups + 7) / 8 * 8 * walks; };
+    hipError_t e = hipSuccess;
+    if (dq.n_segs > 1) {
+        static bool raised[kMaxLdsDevices] = {};
+        a.workgroups = pairs * (dq.n_segs - 1);
+        e = launch_kernel(linear_backward_kernel<M, DK, NW, true, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(1, true), a, stream);
+        if (e == hipSuccess && dq.scanned) e = launch_scan<M, DK, NW>(dq, stream);
+        if (e == hipSuccess && dq.scanned) e = launch_scan<M, DK, NW>(dk, stream);
+        if (e != hipSuccess) return e;
+    }
+    a.workgroups = pairs * dq.n_segs;
+    if (dv_alike) {
+        static bool raised[kMaxLdsDevices] = {};
+        return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 3>, raised, grid(3), SH::NT, SH::lds_bytes(PIECES, false), a, stream);
+    }
+    static bool raised[kMaxLdsDevices] = {};
+    return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(PIECES, false), a, stream);
+}
+template <class M, int DK>
+hipError_t launch_backward_dk(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream)
+{
+    const bool narrow = dq.dv <= 64, grouped = dq.n_q > 1;
+    if (grouped) return narrow ? launch_backward<M, DK, 4, true>(dq, dk, dv, dv_alike, stream) : launch_backward<M, DK, 8, true>(dq, dk, dv, dv_alike, stream);
+    return narrow ? launch_backward<M, DK, 4, false>(dq, dk, dv, dv_alike, stream) : launch_backward<M, DK, 8, false>(dq, dk, dv, dv_alike, stream);
+}
+// dv alone
+template <class M, int DK>
+hipError_t launch_values_dk(const LinearWalkArgs &a, hipStream_t stream)
+{
+    constexpr int PIECES = M::BF16 ? 2 : 1, VW = M::BF16 ? 3 : 1;
+    const bool narrow = a.dv <= 64;
+    if (a.n_src > 1) return narrow ? launch_one<M, DK, 4, PIECES, VW, false, kSources, true>(a, stream)
+                                  : launch_one<M, DK, 8, PIECES, VW, false, kSources, true>(a, stream);
+    return narrow ? launch_one<M, DK, 4, PIECES, VW, false, kOne, true>(a, stream)
+                                  : launch_one<M, DK, 8, PIECES, VW, false, kOne, true>(a, stream);
 }
 
 }  // namespace linear
