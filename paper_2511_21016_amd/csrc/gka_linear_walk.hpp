@@ -782,7 +782,8 @@ void linear_backward_kernel(LinearBackwardArgs a)
     constexpr int EXACT = M::BF16 ? 3 : 1, PLAIN = M::BF16 ? 2 : 1;
     const int role = blockIdx.x / 8 % WALKS, workgroup = blockIdx.x / (8 * WALKS) * 8 + blockIdx.x % 8;
     if (workgroup >= a.workgroups) return;
-    if (role == 0) walk<M, DK, NW, SUMMARY ? 1 : EXACT, EXACT, !SUMMARY, SUMMARY, GROUPED && !SUMMARY ? kQueries : kOne>(a.walk[0], workgroup);
+    if (!GROUPED && role <= 1) walk<M, DK, NW, SUMMARY ? 1 : EXACT, EXACT, !SUMMARY, SUMMARY, kOne>(a.walk[role], workgroup);
+    else if (role == 0) walk<M, DK, NW, SUMMARY ? 1 : EXACT, EXACT, !SUMMARY, SUMMARY, GROUPED && !SUMMARY ? kQueries : kOne>(a.walk[0], workgroup);
     else if (role == 1) walk<M, DK, NW, SUMMARY ? 1 : EXACT, EXACT, !SUMMARY, SUMMARY, GROUPED ? kSources : kOne>(a.walk[1], workgroup);
     else if constexpr (WALKS == 3) walk<M, DK, NW, PLAIN, EXACT, false, false, GROUPED ? kSources : kOne, true>(a.walk[2], workgroup);
 }
