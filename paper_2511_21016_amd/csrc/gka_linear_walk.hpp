@@ -148,21 +148,41 @@ __device__ __forceinline__ typename M::frag col_frag(const unsigned char *tile, 
     }
 }
 
-// VEC floats as pieces of operand precision; all of them together hold 8 bits per piece (float32 operands: one piece, exact).
+// VEC floats as pieces of operand precision; all of them together hold 8 bits per piece (float32 operands: one piece, exact). What a
+// piece leaves over is x - piece, exact in float32: one dot product of the packed pair with (-1, 0) or (0, -1), added to x, instead
+// of an unpacking and a subtraction for each element. (The factors come from registers: as a literal, (0, -1) has the bits of
+// the inline constant -1.0, which the instruction reads otherwise. As assembly, because the compiler only knows the form that
+// overwrites x and copies x first. Waits: other instructions may read a dot product's result three states later, hence the
+// s_nop; none is needed where x comes from a matrix instruction, because the packing before has read the same registers.)
 template <class M, int N>
 __device__ __forceinline__ void cut(const float *x, typename M::frag (&f)[N])
 {
-    float rest[M::VEC];
+    if constexpr (!M::BF16) {
+        static_assert(N == 1, "float32 operands are not cut");
+        f[0] = x[0];
+    } else {
+        uint32_t first = 0x0000bf80u, second = 0xbf800000u;
+        asm("" : "+s"(first), "+s"(second));
+        float rest[8];
 #pragma unroll
-    for (int e = 0; e < M::VEC; ++e) rest[e] = x[e];
+        for (int e = 0; e < 8; ++e) rest[e] = x[e];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        f[i] = M::pack(rest);
-        if (i + 1 < N) {
-            float back[M::VEC];
-            M::unpack(f[i], back);
+        for (int i = 0; i < N; ++i) {
+            f[i] = M::pack(rest);
+            if (i + 1 < N) {
+                const u32x4_t pairs = __builtin_bit_cast(u32x4_t, f[i]);
+                float left[8];
+                asm("v_dot2_f32_bf16 %0, %8, %12, %14\n\tv_dot2_f32_bf16 %1, %8, %13, %15\n\t"
+                    "v_dot2_f32_bf16 %2, %9, %12, %16\n\tv_dot2_f32_bf16 %3, %9, %13, %17\n\t"
+                    "v_dot2_f32_bf16 %4, %10, %12, %18\n\tv_dot2_f32_bf16 %5, %10, %13, %19\n\t"
+                    "v_dot2_f32_bf16 %6, %11, %12, %20\n\tv_dot2_f32_bf16 %7, %11, %13, %21\n\ts_nop 2"
+                    : "=&v"(left[0]), "=&v"(left[1]), "=&v"(left[2]), "=&v"(left[3]), "=&v"(left[4]), "=&v"(left[5]), "=&v"(left[6]),
+                      "=&v"(left[7])
+                    : "v"(pairs[0]), "v"(pairs[1]), "v"(pairs[2]), "v"(pairs[3]), "s"(first), "s"(second), "v"(rest[0]), "v"(rest[1]),
+                      "v"(rest[2]), "v"(rest[3]), "v"(rest[4]), "v"(rest[5]), "v"(rest[6]), "v"(rest[7]));
 #pragma unroll
-            for (int e = 0; e < M::VEC; ++e) rest[e] -= back[e];
+                for (int e = 0; e < 8; ++e) rest[e] = left[e];
+            }
         }
     }
 }
@@ -273,24 +293,28 @@ struct StateAt {
     }
 };
 
-// One chunk's rows of one head as a raw buffer: reads of tokens and features that do not exist give zeros and writes to them are
-// dropped by the buffer's bounds, without a branch. `lane` offsets (chunk_row below) count from the first row of the buffer.
-struct ChunkRows {
-    buffer_rsrc rows;
-    int top;                                       // byte offset of the walk's first token of the chunk
-};
-// ES: bytes of an element. Rows are at most 2^23 elements apart, so that a chunk's bytes stay below 2^30.
+// The rows of one head chunk by chunk, each chunk's a raw buffer: reads of tokens and features that do not exist give zeros and writes
+// to them are dropped by the buffer's bounds, without a branch. `lane` offsets (chunk_offset below) count from the first row of
+// the buffer. Rows are below 2^23 elements apart, so that a chunk's bytes stay below 2^30.
 template <int C, int ES>
-__device__ __forceinline__ ChunkRows chunk_rows(const RowTensor &x, int b, int head, int tau0, int T, int reverse)
-{
-    const int left = T - tau0;                     // tokens of the walk from here on
-    const int count = left < C ? left : C;
-    const int lowest = reverse ? left - count : tau0;
-    const char *base = (const char *)x.p + (b * x.sb + lowest * x.st + head * x.sh) * ES;
-    const int pitch = (int)x.st * ES;
-    return {__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, count * pitch, 0x00020000), reverse ? (count - 1) * pitch : 0};
-}
-// Offset of feature `col` of the chunk's row `row` but for ChunkRows::top; far outside for a feature that does not exist. A token
+struct ChunkRows {
+    const char *base;                              // lowest row of a whole chunk (of the last one it may lie before the tensor)
+    int pitch;                                     // bytes
+    __device__ __forceinline__ ChunkRows(const RowTensor &x, int b, int head, int chunk, int T, int reverse)
+    {
+        pitch = (int)x.st * ES;
+        base = (const char *)x.p + (b * x.sb + head * x.sh) * ES + (int64_t)(reverse ? T - C - chunk * C : chunk * C) * pitch;
+    }
+    __device__ __forceinline__ void next(int reverse) { base += (int64_t)(reverse ? -C : C) * pitch; }
+    // count: tokens of the chunk (0: an empty buffer); head: bytes to a further head
+    __device__ __forceinline__ buffer_rsrc rows(int count, int reverse, int64_t head = 0) const
+    {
+        return __builtin_amdgcn_make_buffer_rsrc((void *)(base + head + (reverse ? (C - count) * pitch : 0)), 0, count * pitch, 0x00020000);
+    }
+    // byte offset of the walk's first token of the chunk
+    __device__ __forceinline__ int top(int count, int reverse) const { return reverse ? (count - 1) * pitch : 0; }
+};
+// Offset of feature `col` of the chunk's row `row` but for ChunkRows::top(); far outside for a feature that does not exist. A token
 // behind the last one lies behind the buffer's end or, in reverse, at a negative offset, which counts as one of 2^31 or more.
 template <int ES>
 __device__ __forceinline__ int chunk_offset(const RowTensor &x, int row, int col, bool exists, int reverse)
@@ -342,7 +366,7 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     constexpr int LOOKAHEAD = ROOMY ? 4 : GROUP == kSources ? 1 : 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char *sK = smem, *sV = smem + SH::k_bytes;
-    float *tables = (float *)(sV + SH::v_bytes);   // [2][5][64]: log2 decay (two floats), weight in the state, zeta of a token; zeta_C
+    float *tables = (float *)(sV + SH::v_bytes);   // [2][5][64]: log2 decay (two floats), weight in the state, zeta of a token (both with the state's factor); that factor
     unsigned char *sQ = (unsigned char *)tables + SH::tables, *sP = sQ + SH::q_bytes;
 
     const int tid = threadIdx.x;
@@ -371,27 +395,31 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     const int v_off = chunk_offset<ES>(a.v, tid / VROW, v0 + E * (tid % VROW), v0 + E * (tid % VROW) < a.dv, a.reverse);
     // (chunks behind the segment: an empty buffer, zeros without a read. Every path writes the registers, so that they are not
     // held from where they are staged to where the next rows are asked for.)
-    auto fetch_rows = [&](auto &to, const RowTensor &x, int head, int tau0, bool exists, int offset, int rows_per) {
-        const ChunkRows r = chunk_rows<C, ES>(x, b, head, exists ? tau0 : 0, exists ? a.T : 0, a.reverse);
-        const int step = chunk_offset<ES>(x, rows_per, 0, true, a.reverse);
+    typedef ChunkRows<C, ES> Tokens;
+    Tokens q_rows(a.q, b, h * (GROUP == kQueries ? steps : 1), chunk_begin, a.T, a.reverse);
+    Tokens k_rows(a.k, b, h * (GROUP == kSources ? steps : 1), chunk_begin, a.T, a.reverse);
+    Tokens v_rows(a.v, b, h * (GROUP == kSources ? steps : 1), chunk_begin, a.T, a.reverse);
+    auto count_of = [&](int c) { return c < chunk_end ? min(C, a.T - c * C) : 0; };
+    auto fetch_rows = [&](auto &to, const Tokens &x, int64_t head, int count, int offset, int rows_per) {
+        const buffer_rsrc rows = x.rows(count, a.reverse, head);
+        const int top = x.top(count, a.reverse), step = (a.reverse ? -rows_per : rows_per) * x.pitch;
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(to) / 16); ++i)
-            to[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r.rows, offset + (r.top + i * step), 0, 0));
+            to[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, offset + (top + i * step), 0, 0));
     };
     auto no_rows = [&](auto &to) {
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(to) / 16); ++i) to[i] = u32x4_t{0, 0, 0, 0};
     };
-    auto fetch = [&](Rows &f, int c, int s) {
-        const bool exists = c < chunk_end;
+    // (of the chunk that q_rows, k_rows and v_rows stand at)
+    auto fetch = [&](Rows &f, int count, int s) {
         if constexpr (!SUMMARY) {
-            if (GROUP == kQueries || s == 0) fetch_rows(f.q, a.q, GROUP == kQueries ? h * steps + s : h, c * C, exists, q_off, NT / KROW);
+            if (GROUP == kQueries || s == 0) fetch_rows(f.q, q_rows, GROUP == kQueries ? s * a.q.sh * ES : 0, count, q_off, NT / KROW);
             else no_rows(f.q);
         }
         if (GROUP == kSources || s == 0) {
-            const int head = GROUP == kSources ? h * steps + s : h;
-            fetch_rows(f.k, a.k, head, c * C, exists, k_off, NT / KROW);
-            fetch_rows(f.v, a.v, head, c * C, exists, v_off, NT / VROW);
+            fetch_rows(f.k, k_rows, GROUP == kSources ? s * a.k.sh * ES : 0, count, k_off, NT / KROW);
+            fetch_rows(f.v, v_rows, GROUP == kSources ? s * a.v.sh * ES : 0, count, v_off, NT / VROW);
         } else {
             no_rows(f.k);
             no_rows(f.v);
@@ -423,8 +451,10 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     const int q_lane = q_place<QT>(lane), k_lane = k_place<M, KT>(lane), kt_lane = col_place<M, KT>(lane);
     const int v_lane = VT::further(col_place<M, VT>(lane), w * (16 * ES / 16));
 
-    // ---- decays: the last wave leaves those of the next chunk in the tables, lane j those of token j
-    float gate = 1.0f, seg_decay = 1.0f;
+    // ---- decays: the last wave leaves those of the next chunk in the tables, lane j those of token j. The state is kept up to a
+    // factor, `scale`, which takes up the chunks' decays; only where it gets small are the registers multiplied by it (table[256];
+    // 1: not in this chunk), instead of all of them in every chunk.
+    float gate = 1.0f, seg_decay = 1.0f, scale = 1.0f;
     auto fetch_gate = [&](int c) {
         const int tau = c * C + lane;
         gate = 1.0f;
@@ -434,17 +464,20 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     auto decays = [&](int c) {
         const double G = wave_inclusive_scan_f64(log2_gate_f64(gate)), total = lane63_f64(G);
         const float hi = (float)G, zeta_C = __builtin_amdgcn_exp2f((float)total);
+        const float after = scale * zeta_C;
+        const bool small = after < 0x1p-16f;
         float *t = tables + (c & 1) * 320 + lane;
         t[0] = hi;
         t[64] = (float)(G - (double)hi);
-        t[128] = c * C + lane < a.T ? __builtin_amdgcn_exp2f((float)(total - G)) : 0.0f;
-        t[192] = __builtin_amdgcn_exp2f(hi);
-        t[256] = zeta_C;
+        t[128] = c * C + lane < a.T ? __builtin_amdgcn_exp2f((float)(total - G)) * (small ? 1.0f : 1.0f / after) : 0.0f;
+        t[192] = __builtin_amdgcn_exp2f(hi) * scale;
+        scale = small ? 1.0f : after;
+        t[256] = lane == 0 ? (small ? after : 1.0f) : scale;
         seg_decay *= zeta_C;
     };
 
     Rows rows;
-    fetch(rows, chunk_begin, 0);
+    fetch(rows, count_of(chunk_begin), 0);
     if (w == NW - 1) fetch_gate(chunk_begin);
 
     // ---- the state that the segment starts from
@@ -481,19 +514,27 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
         }
     }
 
+    Tokens y_rows(a.y, b, h * (GROUP == kQueries ? steps : 1), chunk_begin, a.T, a.reverse);
+    Tokens dot_rows(a.dot_with, b, h * (GROUP == kQueries ? steps : 1), chunk_begin, a.T, a.reverse);
     if (w == NW - 1) {
         decays(chunk_begin);
         fetch_gate(chunk_begin + 1);
     }
     for (int c = chunk_begin; c < chunk_end; ++c) {
         const float *sHi = tables + (c & 1) * 320, *sLo = sHi + 64, *sW = sHi + 128, *sZ = sHi + 192;
+        const int count = count_of(c);
         f32x4 y[TB];
         for (int s = 0; s < steps; ++s) {
             lds_barrier();                         // the tiles of the step before have been read
             stage(rows, s);
             auto fetch_next = [&] {
                 const bool more = GROUP != kOne && s + 1 < steps;
-                fetch(rows, more ? c : c + 1, more ? s + 1 : 0);
+                if (!more) {
+                    q_rows.next(a.reverse);
+                    k_rows.next(a.reverse);
+                    v_rows.next(a.reverse);
+                }
+                fetch(rows, count_of(more ? c : c + 1), more ? s + 1 : 0);
             };
             if (SUMMARY || ROOMY) fetch_next();
             lds_barrier();                         // (no wait for the rows in flight)
@@ -510,7 +551,8 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                 const int lane = anew(lane0), n = lane & 15, kg = lane >> 4;
                 for (int unit = w; unit < SH::UNITS; unit += NW) {
                     const int tb = unit < 2 ? unit : 1 + unit / 2, sb = unit < 2 ? 0 : unit & 1;
-                    f32x4 x[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+                    const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                    f32x4 x[2];
                     constexpr int PB = !BF16 ? 1 : KB < LOOKAHEAD ? KB : LOOKAHEAD;        // 32-blocks of features in flight
                     frag qf[PB][STEPS], kf[2][PB][STEPS];
 #pragma unroll
@@ -528,21 +570,25 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                         for (int kb = 0; kb < PB; ++kb)
 #pragma unroll
                             for (int st = 0; st < STEPS; ++st) {
-                                x[0] = M::mma(kf[0][kb][st], qf[kb][st], x[0]);
-                                x[1] = M::mma(kf[1][kb][st], qf[kb][st], x[1]);
+                                x[0] = M::mma(kf[0][kb][st], qf[kb][st], k0 + kb + st == 0 ? zero : x[0]);
+                                x[1] = M::mma(kf[1][kb][st], qf[kb][st], k0 + kb + st == 0 ? zero : x[1]);
                             }
                     }
-                    // register r: key 32 sb + 16 half + 4 kg + r, token 16 tb + n
+                    // register r: key 32 sb + 16 half + 4 kg + r, token 16 tb + n. (Where an output is bf16, the second float of the decays is
+                    // left out: it is below 2^-18 unless the chunk holds wiped states, 2^-11 with a wiped one at every token.)
                     const float hi = sHi[16 * tb + n], lo = sLo[16 * tb + n];
                     float m[8];
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const int s0 = 32 * sb + 16 * half + 4 * kg;
-                        const f32x4 h4 = *(const f32x4 *)(sHi + s0), l4 = *(const f32x4 *)(sLo + s0);
+                        const int s0 = 32 * sb + 16 * half + 4 * kg, below = tb - 2 * sb - half;
+                        f32x4 d = hi - *(const f32x4 *)(sHi + s0);
+                        if constexpr (!BF16 || PIECES > 2) d += lo - *(const f32x4 *)(sLo + s0);
+                        if (below == 0) {                      // (behind the token: 2^-1000 = 0)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            // (behind the token: 2^-1000 = 0; the select before the exp2 leaves no branch)
-                            m[4 * half + r] = x[half][r] * __builtin_amdgcn_exp2f(s0 + r <= 16 * tb + n ? (hi - h4[r]) + (lo - l4[r]) : -1000.0f);
+                            for (int r = 0; r < 4; ++r) d[r] = 4 * kg + r <= n ? d[r] : -1000.0f;
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) m[4 * half + r] = below < 0 ? 0.0f : x[half][r] * __builtin_amdgcn_exp2f(d[r]);
                     }
 #pragma unroll
                     for (int st = 0; st < STEPS; ++st) {
@@ -621,21 +667,22 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                 // ---- out: register r holds feature v0 + 16 w + 4 kg + r of token 16 tb + n
                 if (GROUP == kQueries || s + 1 == steps) {
                     const int lane = anew(lane0), n = lane & 15, kg = lane >> 4;
-                    const int head = GROUP == kQueries ? h * steps + s : h;
+                    const int64_t to_head = GROUP == kQueries ? s : 0;
                     const int col = v0 + 16 * w + 4 * kg;
                     const bool in = v0 + 16 * w < a.dv;
                     if constexpr (DOT) {
                         float *sDot = (float *)sP; // [NW][C], in place of the masked products
-                        const ChunkRows r = chunk_rows<C, ES>(a.dot_with, b, head, c * C, a.T, a.reverse);
+                        const buffer_rsrc with = dot_rows.rows(count, a.reverse, to_head * a.dot_with.sh * ES);
+                        const int top = dot_rows.top(count, a.reverse);
                         lds_barrier();
 #pragma unroll
                         for (int tb = 0; tb < TB; ++tb) {
-                            const int at = chunk_offset<ES>(a.dot_with, 16 * tb + n, col, in, a.reverse) + r.top;
+                            const int at = chunk_offset<ES>(a.dot_with, 16 * tb + n, col, in, a.reverse) + top;
                             f32x4 x;
                             if constexpr (BF16)
-                                x = IOBF16::cvt4(__builtin_bit_cast(u16x4, __builtin_amdgcn_raw_buffer_load_b64(r.rows, at, 0, 0)));
+                                x = IOBF16::cvt4(__builtin_bit_cast(u16x4, __builtin_amdgcn_raw_buffer_load_b64(with, at, 0, 0)));
                             else
-                                x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r.rows, at, 0, 0));
+                                x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(with, at, 0, 0));
                             float dot = 0.0f;
 #pragma unroll
                             for (int e = 0; e < 4; ++e) dot += x[e] * y[tb][e];
@@ -651,7 +698,8 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                             a.dot_out[((((int64_t)slice * n_pairs + pair) * a.n_q) + (GROUP == kQueries ? s : 0)) * a.T + (a.reverse ? a.T - 1 - tau : tau)] = dot;
                         }
                     }
-                    const ChunkRows out = chunk_rows<C, ES>(a.y, b, head, c * C, a.T, a.reverse);
+                    const buffer_rsrc out = y_rows.rows(count, a.reverse, to_head * a.y.sh * ES);
+                    const int out_top = y_rows.top(count, a.reverse);
                     if constexpr (BF16) {
                         // (lanes of neighbouring kg exchange runs of two token blocks, so that a lane stores eight features at once)
 #pragma unroll
@@ -666,14 +714,14 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                             const auto r0 = __builtin_amdgcn_permlane16_swap(x[0][0], x[1][0], false, false);
                             const auto r1 = __builtin_amdgcn_permlane16_swap(x[0][1], x[1][1], false, false);
                             // even kg: features 4 kg .. + 7 of block tb; odd kg: 4 (kg - 1) .. + 7 of block tb + 1
-                            const int at = chunk_offset<ES>(a.y, 16 * (tb + (kg & 1)) + n, v0 + 16 * w + 4 * (kg & 2), in, a.reverse) + out.top;
-                            __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{r0[0], r1[0], r0[1], r1[1]}, out.rows, at, 0, 0);
+                            const int at = chunk_offset<ES>(a.y, 16 * (tb + (kg & 1)) + n, v0 + 16 * w + 4 * (kg & 2), in, a.reverse) + out_top;
+                            __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{r0[0], r1[0], r0[1], r1[1]}, out, at, 0, 0);
                         }
                     } else {
 #pragma unroll
                         for (int tb = 0; tb < TB; ++tb)
-                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, y[tb]), out.rows,
-                                                                   chunk_offset<ES>(a.y, 16 * tb + n, col, in, a.reverse) + out.top, 0, 0);
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, y[tb]), out,
+                                                                   chunk_offset<ES>(a.y, 16 * tb + n, col, in, a.reverse) + out_top, 0, 0);
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -681,9 +729,11 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
 
             // ---- S <- zeta_C S + sum_s w_s v_s k_s^T
             if (GROUP == kSources ? s == 0 : s + 1 == steps) {
-                const float zeta_C = sHi[256];
+                const float factor = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(sHi[256])));
+                if (factor != 1.0f) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[j] *= zeta_C;
+                    for (int j = 0; j < NJ; ++j) acc[j] *= factor;
+                }
             }
             if (GROUP == kSources || s + 1 == steps) {
                 const int kt_at = anew(kt_lane), kg = anew(lane0) >> 4;
@@ -723,8 +773,15 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                     });
             }
         }
+        if constexpr (!SUMMARY) y_rows.next(a.reverse);
+        if constexpr (DOT) dot_rows.next(a.reverse);
     }
 
+    {
+        const float factor = tables[((chunk_end - 1) & 1) * 320 + 257];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[j] *= factor;
+    }
     if constexpr (SUMMARY) {
         float *s = a.seg_states + seg_state_at(a, pair, slice, seg, state_floats) + (w * NJ * 64 + lane) * 4;
 #pragma unroll
