@@ -378,8 +378,8 @@ typedef struct {
  *           share > 1 (GKA_ERR_SHAPE)
  *   o must not overlap the inputs
  *   workspace: gka_linear_forward_workspace_bytes(p) bytes (0: p is invalid), 256-byte aligned: states and decays of the
- *   segments that the sequences are cut into, at most 1024 of up to 128 KiB or three for each state; contents unspecified
- *   afterwards. */
+ *   segments that the sequences are cut into, up to 1024 of up to 128 KiB unless walk_chunks asks for more; contents
+ *   unspecified afterwards. */
 size_t gka_linear_forward_workspace_bytes(const gka_linear_params *p);
 gka_status gka_linear_forward(const gka_linear_params *p,
                               const void *q, const void *k, const void *v, const float *gate,

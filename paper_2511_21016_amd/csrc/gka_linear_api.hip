@@ -8,8 +8,8 @@ namespace {
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-// Segments are added up to this many workgroups of a walk: two on each CU.
-constexpr int64_t kWalkWorkgroups = 2 * gka::kComputeUnits;
+// A walk is cut into segments up to this many workgroups of it: four for each CU, two of which run at a time.
+constexpr int64_t kWalkWorkgroups = 4 * gka::kComputeUnits;
 
 // Up to this many segments a walk adds up the states of those before it by itself; above, a launch between does.
 constexpr int kMostSegmentsAddedUp = 16;
@@ -88,22 +88,54 @@ struct WalkPlan {
     size_t state_bytes, decay_bytes;   // of the segments' states and decays in the workspace
 };
 
+// What a pass does over its chunks: `walks` walks in one launch, each chunk at walk_cost, after `summaries` in another, at summary_cost
+// (in times of a chunk of the forward pass's summary, 1.7 us at d 128).
+struct PassCost {
+    int walks, summaries;
+    float walk_cost, summary_cost;
+};
+PassCost forward_cost(int G) { return {1, 1, 1.9f + 0.85f * G, 1.0f}; }
+PassCost backward_cost(int G) { return {3, 2, 2.4f + 1.1f * G, 1.3f}; }
+
+// Chunks of a segment, of `states` states of `chunks` chunks: the number whose estimated time is shortest. A chunk costs a CU the same
+// whether one or two workgroups share it, so a launch takes ceil(workgroups / 256) segments' times, and the most segments for each
+// such number are the candidates; the summaries walk all segments but the last once more; starting workgroups, the launches and adding
+// up the states before a segment (above kMostSegmentsAddedUp: the scan) cost the rest. Measured, us, by chunks of a segment: 64 states
+// x 4096 tokens, forward pass 8: 96, 16: 98, 32: 196, backward pass 8: 346, 16: 327; 8 states x 4 heads x 32768 tokens 8: 249, 16: 258,
+// 32: 640; backward pass of 8 states x 3 heads x 1337 tokens 1: 77, 2: 81, 3: 103; float32, 16 states x 1001 tokens 1: 44, 2: 28, 4: 37.
+int walk_segment(int64_t states, int64_t chunks, const PassCost &c)
+{
+    const auto rounds = [](int64_t workgroups) { return (float)((workgroups + gka::kComputeUnits - 1) / gka::kComputeUnits); };
+    int64_t best = chunks;
+    float best_time = -1.0f;
+    const auto consider = [&](int64_t segs) {
+        if (segs > chunks) segs = chunks;
+        if (segs > 1 && segs * states > kWalkWorkgroups) return;
+        const int64_t len = (chunks + segs - 1) / segs, n = (chunks + len - 1) / len;
+        const float r = rounds(n * states * c.walks);
+        float time = (r == 1.0f ? 1.08f : 1.0f) * r * len * c.walk_cost + 2.0f + r;   // (one workgroup on a CU: slower)
+        if (n > 1)
+            time += rounds((n - 1) * states * c.summaries) * len * c.summary_cost + 3.5f + (n > kMostSegmentsAddedUp ? 6.0f : 0.4f * n);
+        if (best_time >= 0.0f && time >= best_time) return;
+        best = len;
+        best_time = time;
+    };
+    consider(1);
+    consider(kMostSegmentsAddedUp);
+    for (int r = 1; r <= c.walks * (int)(kWalkWorkgroups / gka::kComputeUnits); ++r) {
+        const int64_t segs = r * gka::kComputeUnits / (states * c.walks);
+        if (segs > 1) consider(segs);
+    }
+    return (int)best;
+}
+
 // slices: of dv, of the walk whose workgroups the segments are counted for (0: of this one).
-gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv, int slices, WalkPlan *w)
+gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv, int slices, const PassCost &cost, WalkPlan *w)
 {
     w->shape = gka::linear_shape(s.bf16, dk, dv);
     const int64_t chunks = ((int64_t)p->T + w->shape.chunk - 1) / w->shape.chunk;
-    const int64_t walks = s.pairs * (slices > 0 ? slices : w->shape.slices);
-    int64_t segs = 1;
-    if (p->walk_chunks > 0) {
-        segs = (chunks + p->walk_chunks - 1) / p->walk_chunks;
-        w->seg_chunks = p->walk_chunks < chunks ? p->walk_chunks : (int)chunks;
-    } else {
-        segs = (kWalkWorkgroups + walks - 1) / walks;
-        if (segs > chunks / 2) segs = chunks / 2;
-        if (segs < 1) segs = 1;
-        w->seg_chunks = (int)((chunks + segs - 1) / segs);
-    }
+    if (p->walk_chunks > 0) w->seg_chunks = p->walk_chunks < chunks ? p->walk_chunks : (int)chunks;
+    else w->seg_chunks = walk_segment(s.pairs * (slices > 0 ? slices : w->shape.slices), chunks, cost);
     w->n_segs = (int)((chunks + w->seg_chunks - 1) / w->seg_chunks);
     const int64_t states = s.pairs * w->shape.slices * w->n_segs;
     // (the scan runs state_floats / 1024 workgroups for each state of a walk; three walks are one launch)
@@ -141,9 +173,9 @@ gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
     gka_status e = check(p, Call::kWalk, &b->s);
     if (e != GKA_OK) return e;
     // (the walks of dk and dv have their segments in common)
-    if ((e = plan_walk(p, b->s, p->d_v, p->d_k, 0, &b->q)) != GKA_OK) return e;
+    if ((e = plan_walk(p, b->s, p->d_v, p->d_k, 0, backward_cost(b->s.G), &b->q)) != GKA_OK) return e;
     b->k = b->q;
-    if ((e = plan_walk(p, b->s, p->d_k, p->d_v, b->q.shape.slices, &b->v)) != GKA_OK) return e;
+    if ((e = plan_walk(p, b->s, p->d_k, p->d_v, b->q.shape.slices, backward_cost(b->s.G), &b->v)) != GKA_OK) return e;
     size_t off = 0;
     b->off_q = off; off += b->q.state_bytes + b->q.decay_bytes;
     b->off_k = off; off += b->k.state_bytes + b->k.decay_bytes;
@@ -215,7 +247,7 @@ size_t gka_linear_forward_workspace_bytes(const gka_linear_params *p)
 {
     Sizes s;
     WalkPlan w;
-    if (check(p, Call::kWalk, &s) != GKA_OK || plan_walk(p, s, p->d_k, p->d_v, 0, &w) != GKA_OK) return 0;
+    if (check(p, Call::kWalk, &s) != GKA_OK || plan_walk(p, s, p->d_k, p->d_v, 0, forward_cost(s.G), &w) != GKA_OK) return 0;
     const size_t bytes = w.state_bytes + w.decay_bytes;
     return bytes > 0 ? bytes : 256;
 }
@@ -227,7 +259,7 @@ gka_status gka_linear_forward(const gka_linear_params *p, const void *q, const v
     WalkPlan w;
     gka_status e = check(p, Call::kWalk, &s);
     if (e != GKA_OK) return e;
-    if ((e = plan_walk(p, s, p->d_k, p->d_v, 0, &w)) != GKA_OK) return e;
+    if ((e = plan_walk(p, s, p->d_k, p->d_v, 0, forward_cost(s.G), &w)) != GKA_OK) return e;
     if (!q || !k || !v || !gate || !o) return GKA_ERR_NULL;
     if (misaligned({q, k, v, o, S_init, S_final})) return GKA_ERR_SHAPE;
     if (S_final && S_final == S_init && s.share > 1) return GKA_ERR_SHAPE;   // (states that other sequences still read)
