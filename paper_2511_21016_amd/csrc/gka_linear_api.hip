@@ -138,8 +138,8 @@ gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv,
     else w->seg_chunks = walk_segment(s.pairs * (slices > 0 ? slices : w->shape.slices), chunks, cost);
     w->n_segs = (int)((chunks + w->seg_chunks - 1) / w->seg_chunks);
     const int64_t states = s.pairs * w->shape.slices * w->n_segs;
-    // (the scan runs state_floats / 1024 workgroups for each state of a walk; three walks are one launch)
-    if (states > 0x7fffffff / 4 || s.pairs * w->shape.slices * (w->shape.state_floats / 1024) > 0x7fffffff) return GKA_ERR_SHAPE;
+    // (the scan runs state_floats / 256 workgroups for each state of a walk; three walks are one launch)
+    if (states > 0x7fffffff / 4 || s.pairs * w->shape.slices * (w->shape.state_floats / 256) > 0x7fffffff) return GKA_ERR_SHAPE;
     w->state_bytes = w->n_segs > 1 ? align_up((size_t)states * w->shape.state_floats * sizeof(float), 256) : 0;
     w->decay_bytes = w->n_segs > 1 ? align_up((size_t)s.pairs * w->n_segs * sizeof(float), 256) : 0;
     return GKA_OK;

@@ -25,19 +25,29 @@ __global__ __launch_bounds__(kThreads) void linear_gate_kernel(LinearGateArgs a)
     const int b = pair / a.Hkv, h = pair % a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int t0 = part * kPart + tid * kRun;
+    // (tokens behind the last one read it again, so that all reads are under way at once, and are then left out)
     float gate[kRun];
     double x[kRun];
+    int at[kRun];
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-        const int t = t0 + i;
-        gate[i] = 1.0f;
+        at[i] = min(t0 + i, a.T - 1);
+        gate[i] = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + at[i]) * a.Hkv + h];
         x[i] = 0.0;
-        if (t >= a.T) continue;
-        gate[i] = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + t) * a.Hkv + h];
-        for (int s = 0; s < a.q_slices; ++s)
-            for (int g = 0; g < a.G; ++g) x[i] += (double)a.q_dq[(((int64_t)s * n_pairs + pair) * a.G + g) * a.T + t];
-        for (int s = 0; s < a.k_slices; ++s) x[i] -= (double)a.k_dk[((int64_t)s * n_pairs + pair) * a.T + t];
     }
+    for (int s = 0; s < a.q_slices; ++s)
+        for (int g = 0; g < a.G; ++g)
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) x[i] += (double)a.q_dq[(((int64_t)s * n_pairs + pair) * a.G + g) * a.T + at[i]];
+    for (int s = 0; s < a.k_slices; ++s)
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) x[i] -= (double)a.k_dk[((int64_t)s * n_pairs + pair) * a.T + at[i]];
+#pragma unroll
+    for (int i = 0; i < kRun; ++i)
+        if (t0 + i >= a.T) {
+            gate[i] = 1.0f;
+            x[i] = 0.0;
+        }
     double sum = 0.0;
     int open = 1;
 #pragma unroll
