@@ -187,6 +187,56 @@ __device__ __forceinline__ void cut(const float *x, typename M::frag (&f)[N])
     }
 }
 
+// A wave's v fragments with zeros for infinities and NaN. Returns the first token of the chunk that has one in feature lane % 16 (any
+// number above them all: none), or -1 in all lanes if none of the wave's features has.
+template <class M, int SB>
+__device__ __forceinline__ int without_nonfinite(typename M::frag (&v)[SB][M::STEPS], int lane)
+{
+    // (0 unless one of them is infinite or NaN)
+    float zero = 0.0f;
+#pragma unroll
+    for (int sb = 0; sb < SB; ++sb)
+#pragma unroll
+        for (int st = 0; st < M::STEPS; ++st) {
+            if constexpr (M::BF16) {
+                typedef __bf16 pair_t __attribute__((ext_vector_type(2)));
+                const u32x4_t u = __builtin_bit_cast(u32x4_t, v[sb][st]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t pair = u[e];
+                    zero = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_t, pair), __builtin_bit_cast(pair_t, 0u), zero, false);
+                }
+            } else {
+                zero = __builtin_fmaf(v[sb][st], 0.0f, zero);
+            }
+        }
+    if (__builtin_expect(__ballot(!(zero == 0.0f)) == 0, 1)) return -1;
+    int first = 1 << 20;
+#pragma unroll
+    for (int sb = 0; sb < SB; ++sb)
+#pragma unroll
+        for (int st = 0; st < M::STEPS; ++st) {
+            if constexpr (M::BF16) {
+                u32x4_t u = __builtin_bit_cast(u32x4_t, v[sb][st]);
+#pragma unroll
+                for (int e = 7; e >= 0; --e) {
+                    const uint32_t exponent = e & 1 ? 0x7f800000u : 0x7f80u;
+                    if ((u[e / 2] & exponent) == exponent) {
+                        first = min(first, 32 * sb + 16 * (e >> 2) + (e & 3) + 4 * (lane >> 4));
+                        u[e / 2] &= e & 1 ? 0xffffu : 0xffff0000u;
+                    }
+                }
+                v[sb][st] = __builtin_bit_cast(typename M::frag, u);
+            } else if ((__float_as_uint(v[sb][st]) & 0x7f800000u) == 0x7f800000u) {
+                first = min(first, 32 * sb + 16 * (st >> 2) + (st & 3) + 4 * (lane >> 4));
+                v[sb][st] = 0.0f;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    first = min(first, __shfl_xor(first, 16, 64));
+    return min(first, __shfl_xor(first, 32, 64));
+}
+
 // DK: padded features of q and k. NW: waves, 16 features of v each.
 template <class M, int DK, int NW>
 struct Shape {
@@ -583,12 +633,12 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                         const int s0 = 32 * sb + 16 * half + 4 * kg, below = tb - 2 * sb - half;
                         f32x4 d = hi - *(const f32x4 *)(sHi + s0);
                         if constexpr (!BF16 || PIECES > 2) d += lo - *(const f32x4 *)(sLo + s0);
-                        if (below == 0) {                      // (behind the token: 2^-1000 = 0)
+                        // (keys behind the token are left out by a selection: they may hold anything)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) d[r] = 4 * kg + r <= n ? d[r] : -1000.0f;
+                        for (int r = 0; r < 4; ++r) {
+                            const float product = x[half][r] * __builtin_amdgcn_exp2f(d[r]);
+                            m[4 * half + r] = below < 0 || (below == 0 && 4 * kg + r > n) ? 0.0f : product;
                         }
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) m[4 * half + r] = below < 0 ? 0.0f : x[half][r] * __builtin_amdgcn_exp2f(d[r]);
                     }
 #pragma unroll
                     for (int st = 0; st < STEPS; ++st) {
@@ -641,6 +691,9 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                 for (int st = 0; st < STEPS; ++st) vt[sb][st] = col_frag<M, VT>(sV, v_lane, 0, sb, st);
 
             if constexpr (!SUMMARY) {
+                // Infinities and NaN in v reach the tokens from their own on, in their feature; a product with the zeros of the tokens before
+                // would carry them there too. They leave these products and are put in below, where there are any.
+                const int first_bad = without_nonfinite<M>(vt, lane0);
                 // (asked for only now where registers are few: half a chunk ahead, with none of them held through the products before)
                 if (!ROOMY) fetch_next();
                 lds_barrier();                     // the masked products are there
@@ -664,6 +717,19 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                             y[tb] = M::mma(vt[sb][st], p.f[e], y[tb]);
                         }
                     });
+                if (__builtin_expect(__builtin_amdgcn_readfirstlane(first_bad) >= 0, 0)) {
+                    const int lane = anew(lane0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int from = __shfl(first_bad, 4 * (lane >> 4) + r, 64);
+#pragma unroll
+                        for (int tb = 0; tb < TB; ++tb) y[tb][r] = 16 * tb + (lane & 15) >= from ? __builtin_nanf("") : y[tb][r];
+                    }
+#pragma unroll
+                    for (int sb = 0; sb < SB; ++sb)
+#pragma unroll
+                        for (int st = 0; st < STEPS; ++st) vt[sb][st] = col_frag<M, VT>(sV, v_lane, 0, sb, st);
+                }
                 // ---- out: register r holds feature v0 + 16 w + 4 kg + r of token 16 tb + n
                 if (GROUP == kQueries || s + 1 == steps) {
                     const int lane = anew(lane0), n = lane & 15, kg = lane >> 4;
