@@ -350,12 +350,16 @@ gka_status gka_forward_sketched(const gka_params *p,
  * Tensors of rows: q [B,T,H,d_k], k [B,T,H_kv,d_k], v [B,T,H_kv,d_v], o [B,T,H,d_v], all GKA_F32 or all GKA_BF16, 16-byte
  * aligned; each has element strides of its own. Sums, states and decays are float32 or wider for either type; with bf16
  * tensors what is computed in float32 enters the matrix products as two or three bf16 pieces, so that an output carries the
- * rounding of its own type. */
+ * rounding of its own type. An infinity or NaN in a row of q, k or v reaches the outputs that depend on the row and no others
+ * (rows of a padded batch behind a sequence's end may hold anything); where it reaches, NaN may stand for an infinity.
+ *
+ * Limits: B H_kv < 2^21, B H <= 2^26, T and cache_tokens <= 2^31 - 2^13 (GKA_ERR_SHAPE beyond). Tensors that a call writes overlap
+ * none that it reads, and their rows not each other, unless it is said below. */
 typedef struct {
     int32_t B;            /* sequences                                                                 */
     int32_t H;            /* query heads, a multiple of H_kv                                           */
     int32_t H_kv;         /* key/value heads = states of a sequence                                    */
-    int32_t T;            /* tokens per sequence, any T >= 1 (ignored by gka_linear_decode_shared)     */
+    int32_t T;            /* tokens per sequence, from 1 on (ignored by gka_linear_decode_shared)      */
     int32_t d_k;          /* features of q and k: a multiple of 16 up to 256                           */
     int32_t d_v;          /* features of v and o: likewise                                             */
     int32_t io_dtype;     /* gka_dtype of q, k, v, o                                                   */
@@ -365,7 +369,7 @@ typedef struct {
     int32_t cache_tokens; /* gka_linear_decode_shared: tokens N that a suffix cache has room for       */
     int32_t walk_chunks;  /* gka_linear_forward, _backward: chunks one workgroup walks (0 = the        */
                           /*   library's choice); results depend on it through rounding only           */
-    int32_t reserved;     /* 0                                                                         */
+    int32_t reserved;     /* 0 (GKA_ERR_UNSUPPORTED)                                                   */
     int64_t q_stride[3];  /* element strides of batch, token and head (the features of a row are       */
     int64_t k_stride[3];  /*   contiguous): positive, multiples of 16 bytes, a row or more from head   */
     int64_t v_stride[3];  /*   to head and token to token, below 2^23 from token to token; 0,0,0 = packed */
@@ -376,7 +380,6 @@ typedef struct {
  *   S_init  [B/share,H_kv,d_v,d_k] float32 or NULL (zero); the first gate multiplies it
  *   S_final [B,H_kv,d_v,d_k] float32, written if not NULL: the states after the last token. May be S_init's buffer unless
  *           share > 1 (GKA_ERR_SHAPE)
- *   o must not overlap the inputs
  *   workspace: gka_linear_forward_workspace_bytes(p) bytes (0: p is invalid), 256-byte aligned: states and decays of the
  *   segments that the sequences are cut into, up to 1024 of up to 128 KiB unless walk_chunks asks for more; contents
  *   unspecified afterwards. */
@@ -394,8 +397,8 @@ gka_status gka_linear_forward(const gka_linear_params *p,
  *   dq, dk, dv  io_dtype, packed like q, k, v (written; dk and dv summed over the query heads of a group)
  *   dgate       float32 like gate (written; [H_kv] with gate_per_head: summed over sequences and tokens). Formed as
  *               (<dS_final,S_T> + sum_{s>=t} (q_s . dq_s - k_s . dk_s)) / gamma_t; where a gate wipes the state it is
- *               written as 0 and the sum restarts
- *   dS_init     [B/share,H_kv,d_v,d_k] float32, written if not NULL
+ *               written as 0 and the sum restarts (an infinity or NaN in a row spoils the sum of all tokens before)
+ *   dS_init     [B/share,H_kv,d_v,d_k] float32, written if not NULL; a buffer of its own (GKA_ERR_SHAPE)
  *   Nothing is added up by atomics: results are the same on every run.
  *   workspace: gka_linear_backward_workspace_bytes(p) bytes, 256-byte aligned. */
 size_t gka_linear_backward_workspace_bytes(const gka_linear_params *p);

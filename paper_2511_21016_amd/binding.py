@@ -617,8 +617,8 @@ def linear_workspace(q, k, v, gate, *, backward=False, walk_chunks=0):
 
 def gka_linear_forward(q, k, v, gate, *, S_init=None, return_state=False, workspace=None, out=None, S_final=None,
                        walk_chunks=0):
-    """gka_linear_forward on torch CUDA tensors: q [B,T,H,d_k], k [B,T,H_kv,d_k], v [B,T,H_kv,d_v] (float32 or bfloat16, any
-    strides with contiguous features), gate [B,T,H_kv] float32 or [H_kv] (one decay for each head); S_init: states
+    """gka_linear_forward on torch CUDA tensors: q [B,T,H,d_k], k [B,T,H_kv,d_k], v [B,T,H_kv,d_v] (float32 or bfloat16;
+    contiguous features, other strides positive multiples of 16 bytes), gate [B,T,H_kv] float32 or [H_kv] (one decay for each head); S_init: states
     [B,H_kv,d_v,d_k] float32 to continue from, or [B/F,..]: each is shared by F consecutive sequences. Returns o [B,T,H,d_v],
     with return_state (or a buffer S_final for them) also the states after the last token."""
     load_library()

@@ -14,6 +14,11 @@ constexpr int64_t kWalkWorkgroups = 4 * gka::kComputeUnits;
 // Up to this many segments a walk adds up the states of those before it by itself; above, a launch between does.
 constexpr int kMostSegmentsAddedUp = 16;
 
+// Threads of a launch, in each direction of its grid, have to be fewer.
+constexpr int64_t kGridThreads = (int64_t)1 << 32;
+// Tokens: positions up to two chunks behind the last one, and the end of its part of a sum over the sequence, are 32-bit numbers.
+constexpr int kMaxTokens = 0x7fffe000;
+
 struct Sizes {
     int share, G;
     int64_t pairs;
@@ -47,19 +52,21 @@ gka_status check(const gka_linear_params *p, Call call, Sizes *s)
 {
     if (!p) return GKA_ERR_NULL;
     if (p->B <= 0 || p->H <= 0 || p->H_kv <= 0 || p->H % p->H_kv) return GKA_ERR_SHAPE;
-    if (call != Call::kShared && p->T <= 0) return GKA_ERR_SHAPE;
-    if (call == Call::kShared && p->cache_tokens <= 0) return GKA_ERR_SHAPE;
+    if (call != Call::kShared && (p->T <= 0 || p->T > kMaxTokens)) return GKA_ERR_SHAPE;
+    if (call == Call::kShared && (p->cache_tokens <= 0 || p->cache_tokens > kMaxTokens)) return GKA_ERR_SHAPE;
     if (p->d_k <= 0 || p->d_v <= 0) return GKA_ERR_SHAPE;
     if (p->d_k % 16 || p->d_v % 16 || p->d_k > 256 || p->d_v > 256) return GKA_ERR_UNSUPPORTED;
     if (p->io_dtype != GKA_F32 && p->io_dtype != GKA_BF16) return GKA_ERR_UNSUPPORTED;
     if (p->gate_per_head != 0 && p->gate_per_head != 1) return GKA_ERR_UNSUPPORTED;
     if (p->share < 0 || p->walk_chunks < 0) return GKA_ERR_SHAPE;
+    if (p->reserved != 0) return GKA_ERR_UNSUPPORTED;
     s->share = p->share > 0 ? p->share : 1;
     if (p->B % s->share) return GKA_ERR_SHAPE;
     s->G = p->H / p->H_kv;
     s->pairs = (int64_t)p->B * p->H_kv;
     s->bf16 = p->io_dtype == GKA_BF16;
-    if (s->pairs > (int64_t)1 << 24 || (int64_t)p->B * p->H > (int64_t)1 << 26) return GKA_ERR_SHAPE;
+    // (of decode up to eight workgroups of 256 threads for a state where there are this many, of the shared call one of 512 for 16 heads)
+    if (s->pairs >= (int64_t)1 << 21 || (int64_t)p->B * p->H > (int64_t)1 << 26) return GKA_ERR_SHAPE;
     const int T = call == Call::kShared ? 1 : p->T;
     gka_status e = row_strides(p->q_stride, p, T, p->H, p->d_k, &s->q);
     if (e == GKA_OK) e = row_strides(p->k_stride, p, T, p->H_kv, p->d_k, &s->k);
@@ -138,8 +145,8 @@ gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv,
     else w->seg_chunks = walk_segment(s.pairs * (slices > 0 ? slices : w->shape.slices), chunks, cost);
     w->n_segs = (int)((chunks + w->seg_chunks - 1) / w->seg_chunks);
     const int64_t states = s.pairs * w->shape.slices * w->n_segs;
-    // (the scan runs state_floats / 256 workgroups for each state of a walk; three walks are one launch)
-    if (states > 0x7fffffff / 4 || s.pairs * w->shape.slices * (w->shape.state_floats / 256) > 0x7fffffff) return GKA_ERR_SHAPE;
+    // (three walks of 512 threads are one launch; of the scan, 64 threads for 256 floats, with its 16 segments and more, less)
+    if (states * 3 * 512 >= kGridThreads) return GKA_ERR_SHAPE;
     w->state_bytes = w->n_segs > 1 ? align_up((size_t)states * w->shape.state_floats * sizeof(float), 256) : 0;
     w->decay_bytes = w->n_segs > 1 ? align_up((size_t)s.pairs * w->n_segs * sizeof(float), 256) : 0;
     return GKA_OK;
@@ -179,6 +186,9 @@ gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
     size_t off = 0;
     b->off_q = off; off += b->q.state_bytes + b->q.decay_bytes;
     b->off_k = off; off += b->k.state_bytes + b->k.decay_bytes;
+    // (a thread for four tokens of a state, in parts of 4096; a thread for four floats of the states)
+    if (b->s.pairs * ((p->T + (int64_t)4095) / 4096) * 1024 >= kGridThreads || b->s.pairs * p->d_k * p->d_v / 4 >= kGridThreads)
+        return GKA_ERR_SHAPE;
     const size_t tokens = (size_t)b->s.pairs * p->T;
     b->off_q_dot = off; off += align_up(b->q.shape.slices * tokens * b->s.G * sizeof(float), 256);
     b->off_k_dot = off; off += align_up(b->k.shape.slices * tokens * sizeof(float), 256);
@@ -270,6 +280,8 @@ gka_status gka_linear_forward(const gka_linear_params *p, const void *q, const v
     a.n_q = s.G;
     a.init = S_init; a.share = s.share;
     a.final = S_final;
+    // (the last segment of a sequence may write its state before another one has started: in place only the scan reads the old states)
+    if (S_final && S_final == S_init && a.n_segs > 1) a.scanned = 1;
     return gka::launch_linear_forward(a, s.bf16, (hipStream_t)hip_stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
 }
 
@@ -288,6 +300,7 @@ gka_status gka_linear_backward(const gka_linear_params *p, const void *q, const 
     if (e != GKA_OK) return e;
     if (!q || !k || !v || !gate || !dy || !dq || !dk || !dv || !dgate) return GKA_ERR_NULL;
     if (misaligned({q, k, v, dy, S_init, dS_final, dq, dk, dv, dS_init})) return GKA_ERR_SHAPE;
+    if (dS_init && (dS_init == S_init || dS_init == dS_final)) return GKA_ERR_SHAPE;   // (walks read those while another writes)
     if (!workspace || workspace_bytes < b.total || ((uintptr_t)workspace & 255)) return GKA_ERR_WORKSPACE;
     hipStream_t stream = (hipStream_t)hip_stream;
     char *ws = (char *)workspace;
@@ -344,7 +357,6 @@ gka_status gka_linear_decode(const gka_linear_params *p, const float *S_in, floa
     if (!S_in || !S_out || !q || !k || !v || !gate || !o) return GKA_ERR_NULL;
     if (misaligned({S_in, S_out, q, k, v, o})) return GKA_ERR_SHAPE;
     if (S_in == S_out && s.share > 1) return GKA_ERR_SHAPE;
-    if (s.pairs * 64 > 0x7fffffff) return GKA_ERR_SHAPE;                     // (workgroups, 16 rows of a state or more to each)
     gka::LinearDecodeArgs a = {};
     a.S_in = S_in; a.S_out = S_out;
     a.q = at(q, s.q); a.k = at(k, s.k); a.v = at(v, s.v); a.y = at(o, s.o);

@@ -209,7 +209,7 @@ for device in (0, 1):
             ws = dict(workspace=X, workspace_bytes=binding.linear_forward_workspace_bytes(p))
             assert binding.linear_forward_raw(p, X, X, X, X, X, X, X, **ws) == 0
             ws["workspace_bytes"] = binding.linear_backward_workspace_bytes(p)
-            assert binding.linear_backward_raw(p, X, X, X, X, X, X, X, X, X, X, X, X, **ws) == 0
+            assert binding.linear_backward_raw(p, X, X, X, X, X, X, X, X, X, X, X, 2 * X, **ws) == 0
             assert binding.linear_decode_raw(p, X, X, X, X, X, X, X) == 0
             assert binding.linear_decode_shared_raw(p, X, X, X, X, X, X, X, X, X, X) == 0
 """)
@@ -226,3 +226,50 @@ for device in (0, 1):
                 assert raised.get((c["mangled"], device), 0) >= c["lds"], (c["kernel"], device)
     for name in ("linear_walk_kernel", "linear_scan_kernel", "linear_gate_kernel", "linear_decode_kernel", "linear_shared_kernel"):
         assert any(name in c["mangled"] for c in launches), name
+
+
+def test_sizes_beyond_the_limits_are_refused():
+    longest = 0x7fffe000
+    for call in CALLS:
+        size = "cache_tokens" if call is _shared else "T"
+        for bad in (dict(B=1 << 20), dict(B=1 << 20, H=128, H_kv=1), {size: longest + 1}, {size: 0x7fffffff}):
+            assert call(_p(**bad)) == binding.GKA_ERR_SHAPE, (call, bad)
+        p = _p()
+        p.reserved = 1
+        assert call(p) == binding.GKA_ERR_UNSUPPORTED
+    for states in (dict(S_init=2 * X, dS_init=2 * X), dict(dS_final=2 * X, dS_init=2 * X)):
+        assert _backward(_p(), **states) == binding.GKA_ERR_SHAPE
+
+
+HUGE = [((1 << 21) - 1, 1, 1, 1, 16, 16), (1 << 20, 1, 1, 1, 256, 256), (1 << 20, 1, 1, 5000, 16, 256), (1 << 16, 64, 16, 1, 32, 16),
+        (1, 1, 1, 0x7fffe000, 16, 16), (2, 1, 1, 0x7fffe000, 256, 256), (1 << 15, 1, 1, 100000, 64, 64)]
+
+
+def test_launches_of_huge_sizes_fit_the_grid():
+    calls = record(f"""
+X = 0x10000000
+for B, H, H_kv, T, d_k, d_v in {HUGE}:
+    for walk in (0, 1):
+        p = binding.make_linear_params(B, H, H_kv, T, d_k, d_v, binding.GKA_BF16, cache_tokens=64, walk_chunks=walk)
+        ws = dict(workspace=X, workspace_bytes=1 << 60)
+        allowed = (binding.GKA_OK, binding.GKA_ERR_SHAPE)
+        assert binding.linear_forward_raw(p, X, X, X, X, X, X, X, **ws) in allowed
+        assert binding.linear_backward_raw(p, X, X, X, X, X, X, X, X, X, X, X, 2 * X, **ws) in allowed
+        assert binding.linear_decode_raw(p, X, X, X, X, X, X, X) == 0
+        assert binding.linear_decode_shared_raw(p, X, X, X, X, X, X, X, X, X, X) == 0
+""")
+    launches = [c for c in calls if c["kind"] == "launch"]
+    assert launches
+    for c in launches:
+        assert 0 < c["grid"] and c["grid"] * c["block"] < 1 << 32, c
+
+
+def test_states_in_place_go_through_the_scan():
+    """With several segments the last one may end before another has started: the old states are then read by the scan alone."""
+    source = """
+X = 0x10000000
+p = binding.make_linear_params(2, 2, 2, 200, 64, 64, binding.GKA_BF16, walk_chunks=1)
+assert binding.linear_forward_raw(p, X, X, X, X, X, 2 * X, {final}, workspace=X, workspace_bytes=1 << 40) == 0
+"""
+    scans = lambda final: sum("linear_scan_kernel" in c["mangled"] for c in record(source.format(final=final)) if c["kind"] == "launch")
+    assert scans("2 * X") == 1 and scans("3 * X") == 0
