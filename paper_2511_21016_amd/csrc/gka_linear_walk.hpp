@@ -255,10 +255,10 @@ struct Shape {
     static constexpr size_t unit_bytes = M::STEPS * 64 * sizeof(typename M::frag);
     static constexpr size_t tables = 2 * 5 * 64 * sizeof(float);
     static constexpr size_t dot_bytes = (size_t)NW * C * sizeof(float);
-    static constexpr size_t p_bytes(int pieces) { return UNITS * unit_bytes * pieces > dot_bytes ? UNITS * unit_bytes * pieces : dot_bytes; }
-    static constexpr size_t lds_bytes(int pieces, bool summary)
+    static constexpr size_t p_bytes(int pieces) { return UNITS * unit_bytes * pieces; }
+    static constexpr size_t lds_bytes(int pieces, bool summary, bool dot)
     {
-        return k_bytes + v_bytes + tables + (summary ? 0 : q_bytes + p_bytes(pieces));
+        return k_bytes + v_bytes + tables + (summary ? 0 : q_bytes + p_bytes(pieces) + (dot ? dot_bytes : 0));
     }
     static_assert((C * DK / E) % NT == 0 && NT % (DK / E) == 0, "a thread's pieces lie in one column");
 };
@@ -418,6 +418,7 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     unsigned char *sK = smem, *sV = smem + SH::k_bytes;
     float *tables = (float *)(sV + SH::v_bytes);   // [2][5][64]: log2 decay (two floats), weight in the state, zeta of a token (both with the state's factor); that factor
     unsigned char *sQ = (unsigned char *)tables + SH::tables, *sP = sQ + SH::q_bytes;
+    float *sDot = (float *)(sP + SH::p_bytes(PIECES));         // [NW][C]: the waves' parts of the dot products (DOT)
 
     const int tid = threadIdx.x;
     const int lane0 = tid & 63, lane = lane0;
@@ -564,6 +565,17 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
         }
     }
 
+    // dot products of chunk c (query s), whose parts lie in LDS since the step before: the same barriers serve both. A wave without decays
+    // and with the fewest masked products does this.
+    auto add_dots = [&](int c, int s) {
+        const int lane = anew(lane0), tau = c * C + lane;
+        if (w != NW - 2 || lane >= C || tau >= a.T) return;
+        float dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) dot += sDot[i * C + lane];
+        a.dot_out[(((int64_t)slice * n_pairs + pair) * a.n_q + s) * a.T + (a.reverse ? a.T - 1 - tau : tau)] = dot;
+    };
+
     Tokens y_rows(a.y, b, h * (GROUP == kQueries ? steps : 1), chunk_begin, a.T, a.reverse);
     Tokens dot_rows(a.dot_with, b, h * (GROUP == kQueries ? steps : 1), chunk_begin, a.T, a.reverse);
     if (w == NW - 1) {
@@ -576,6 +588,10 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
         f32x4 y[TB];
         for (int s = 0; s < steps; ++s) {
             lds_barrier();                         // the tiles of the step before have been read
+            if constexpr (DOT) {
+                if (GROUP == kQueries && s > 0) add_dots(c, s - 1);
+                else if (s == 0 && c > chunk_begin) add_dots(c - 1, GROUP == kQueries ? steps - 1 : 0);
+            }
             stage(rows, s);
             auto fetch_next = [&] {
                 const bool more = GROUP != kOne && s + 1 < steps;
@@ -694,6 +710,21 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                 // Infinities and NaN in v reach the tokens from their own on, in their feature; a product with the zeros of the tokens before
                 // would carry them there too. They leave these products and are put in below, where there are any.
                 const int first_bad = without_nonfinite<M>(vt, lane0);
+                // (rows of the dot products: before the next chunk's, which are not waited for with them)
+                std::conditional_t<BF16, u32x2_t, u32x4_t> dot_row[DOT ? TB : 1];
+                if constexpr (DOT) {
+                    if (GROUP == kQueries || s + 1 == steps) {
+                        const int lane = anew(lane0), n = lane & 15, kg = lane >> 4;
+                        const buffer_rsrc with = dot_rows.rows(count, a.reverse, (GROUP == kQueries ? s : 0) * a.dot_with.sh * ES);
+                        const int top = dot_rows.top(count, a.reverse);
+#pragma unroll
+                        for (int tb = 0; tb < TB; ++tb) {
+                            const int at = chunk_offset<ES>(a.dot_with, 16 * tb + n, v0 + 16 * w + 4 * kg, v0 + 16 * w < a.dv, a.reverse) + top;
+                            if constexpr (BF16) dot_row[tb] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(with, at, 0, 0));
+                            else dot_row[tb] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(with, at, 0, 0));
+                        }
+                    }
+                }
                 // (asked for only now where registers are few: half a chunk ahead, with none of them held through the products before)
                 if (!ROOMY) fetch_next();
                 lds_barrier();                     // the masked products are there
@@ -737,31 +768,16 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                     const int col = v0 + 16 * w + 4 * kg;
                     const bool in = v0 + 16 * w < a.dv;
                     if constexpr (DOT) {
-                        float *sDot = (float *)sP; // [NW][C], in place of the masked products
-                        const buffer_rsrc with = dot_rows.rows(count, a.reverse, to_head * a.dot_with.sh * ES);
-                        const int top = dot_rows.top(count, a.reverse);
-                        lds_barrier();
 #pragma unroll
                         for (int tb = 0; tb < TB; ++tb) {
-                            const int at = chunk_offset<ES>(a.dot_with, 16 * tb + n, col, in, a.reverse) + top;
                             f32x4 x;
-                            if constexpr (BF16)
-                                x = IOBF16::cvt4(__builtin_bit_cast(u16x4, __builtin_amdgcn_raw_buffer_load_b64(with, at, 0, 0)));
-                            else
-                                x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(with, at, 0, 0));
+                            if constexpr (BF16) x = IOBF16::cvt4(__builtin_bit_cast(u16x4, dot_row[tb]));
+                            else x = __builtin_bit_cast(f32x4, dot_row[tb]);
                             float dot = 0.0f;
 #pragma unroll
                             for (int e = 0; e < 4; ++e) dot += x[e] * y[tb][e];
                             dot = sum_over_kg(dot);
                             if (kg == 0) sDot[w * C + 16 * tb + n] = dot;
-                        }
-                        lds_barrier();
-                        if (w == 0 && lane < C && c * C + lane < a.T) {
-                            float dot = 0.0f;
-#pragma unroll
-                            for (int i = 0; i < NW; ++i) dot += sDot[i * C + lane];
-                            const int tau = c * C + lane;
-                            a.dot_out[((((int64_t)slice * n_pairs + pair) * a.n_q) + (GROUP == kQueries ? s : 0)) * a.T + (a.reverse ? a.T - 1 - tau : tau)] = dot;
                         }
                     }
                     const buffer_rsrc out = y_rows.rows(count, a.reverse, to_head * a.y.sh * ES);
@@ -843,6 +859,10 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
         if constexpr (DOT) dot_rows.next(a.reverse);
     }
 
+    if constexpr (DOT) {
+        lds_barrier();
+        add_dots(chunk_end - 1, GROUP == kQueries ? steps - 1 : 0);
+    }
     {
         const float factor = tables[((chunk_end - 1) & 1) * 320 + 257];
 #pragma unroll
@@ -961,10 +981,10 @@ template <class M, int DK, int NW, int PIECES, int VW, bool SUMMARY, Group GROUP
 hipError_t launch_one(const LinearWalkArgs &a, hipStream_t stream)
 {
     typedef Shape<M, DK, NW> SH;
-    static_assert(SH::lds_bytes(3, false) <= (size_t)160 << 10, "LDS of a CU");
+    static_assert(SH::lds_bytes(3, false, true) <= (size_t)160 << 10, "LDS of a CU");
     static bool raised[kMaxLdsDevices] = {};
     return launch_kernel(linear_walk_kernel<M, DK, NW, PIECES, VW, SUMMARY, GROUP, TURNED>, raised,
-                         a.B * a.Hkv * a.slices * (SUMMARY ? a.n_segs - 1 : a.n_segs), SH::NT, SH::lds_bytes(PIECES, SUMMARY), a, stream);
+                         a.B * a.Hkv * a.slices * (SUMMARY ? a.n_segs - 1 : a.n_segs), SH::NT, SH::lds_bytes(PIECES, SUMMARY, false), a, stream);
 }
 
 template <int DK, int NW>
@@ -1014,17 +1034,17 @@ hipError_t launch_backward(const LinearWalkArgs &dq, const LinearWalkArgs &dk, c
     if (dq.n_segs > 1) {
         static bool raised[kMaxLdsDevices] = {};
         a.workgroups = pairs * (dq.n_segs - 1);
-        e = launch_kernel(linear_backward_kernel<M, DK, NW, true, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(1, true), a, stream);
+        e = launch_kernel(linear_backward_kernel<M, DK, NW, true, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(1, true, false), a, stream);
         if (e == hipSuccess && dq.scanned) e = launch_scan<DK, NW>(a, 2, stream);
         if (e != hipSuccess) return e;
     }
     a.workgroups = pairs * dq.n_segs;
     if (dv_alike) {
         static bool raised[kMaxLdsDevices] = {};
-        return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 3>, raised, grid(3), SH::NT, SH::lds_bytes(PIECES, false), a, stream);
+        return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 3>, raised, grid(3), SH::NT, SH::lds_bytes(PIECES, false, true), a, stream);
     }
     static bool raised[kMaxLdsDevices] = {};
-    return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(PIECES, false), a, stream);
+    return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(PIECES, false, true), a, stream);
 }
 template <class M, int DK>
 hipError_t launch_backward_dk(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream)
