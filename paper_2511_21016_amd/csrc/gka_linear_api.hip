@@ -11,8 +11,16 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // A walk is cut into segments up to this many workgroups of it: four for each CU, two of which run at a time.
 constexpr int64_t kWalkWorkgroups = 4 * gka::kComputeUnits;
 
-// Up to this many segments a walk adds up the states of those before it by itself; above, a launch between does.
+// Up to this many segments a walk adds up the states of those before it by itself; above, a launch between (the scan) does. The three
+// walks of the backward pass, one of which reads the states transposed, add up 65536 floats at most, or 4 segments. Measured, us, added
+// up against scanned: forward pass, 8 states of 128 x 128, 16 segments 19.6 : 23.4; backward pass 54.6 : 41.5, 8 segments 40.8 : 38.6,
+// 16 such states, 16 segments 88 : 67; 16 states of 64 x 64, 16 segments 45.6 : 49.8; of 256 x 128, 12 segments 138 : 106, 5 81 : 83.
 constexpr int kMostSegmentsAddedUp = 16;
+int most_added_up_backward(int64_t state_floats)
+{
+    const int64_t segs = 65536 / state_floats;
+    return segs < 4 ? 4 : segs > kMostSegmentsAddedUp ? kMostSegmentsAddedUp : (int)segs;
+}
 
 // Threads of a launch, in each direction of its grid, have to be fewer.
 constexpr int64_t kGridThreads = (int64_t)1 << 32;
@@ -92,22 +100,23 @@ gka::RowTensor at(const void *p, gka::RowTensor strides)
 struct WalkPlan {
     gka::LinearShape shape;
     int n_segs, seg_chunks;
+    bool scanned;                      // the scan adds up the segments' states
     size_t state_bytes, decay_bytes;   // of the segments' states and decays in the workspace
 };
 
 // What a pass does over its chunks: `walks` walks in one launch, each chunk at walk_cost, after `summaries` in another, at summary_cost
 // (in times of a chunk of the forward pass's summary, 1.7 us at d 128).
 struct PassCost {
-    int walks, summaries;
+    int walks, summaries, most_added_up;
     float walk_cost, summary_cost;
 };
-PassCost forward_cost(int G) { return {1, 1, 1.9f + 0.85f * G, 1.0f}; }
-PassCost backward_cost(int G) { return {3, 2, 2.4f + 1.1f * G, 1.3f}; }
+PassCost forward_cost(int G) { return {1, 1, kMostSegmentsAddedUp, 1.9f + 0.85f * G, 1.0f}; }
+PassCost backward_cost(int G, int64_t state_floats) { return {3, 2, most_added_up_backward(state_floats), 2.4f + 1.1f * G, 1.3f}; }
 
 // Chunks of a segment, of `states` states of `chunks` chunks: the number whose estimated time is shortest. A chunk costs a CU the same
 // whether one or two workgroups share it, so a launch takes ceil(workgroups / 256) segments' times, and the most segments for each
 // such number are the candidates; the summaries walk all segments but the last once more; starting workgroups, the launches and adding
-// up the states before a segment (above kMostSegmentsAddedUp: the scan) cost the rest. Measured, us, by chunks of a segment: 64 states
+// up the states before a segment, or the scan, cost the rest. Measured, us, by chunks of a segment: 64 states
 // x 4096 tokens, forward pass 8: 96, 16: 98, 32: 196, backward pass 8: 346, 16: 327; 8 states x 4 heads x 32768 tokens 8: 249, 16: 258,
 // 32: 640; backward pass of 8 states x 3 heads x 1337 tokens 1: 77, 2: 81, 3: 103; float32, 16 states x 1001 tokens 1: 44, 2: 28, 4: 37.
 int walk_segment(int64_t states, int64_t chunks, const PassCost &c)
@@ -122,13 +131,13 @@ int walk_segment(int64_t states, int64_t chunks, const PassCost &c)
         const float r = rounds(n * states * c.walks);
         float time = (r == 1.0f ? 1.08f : 1.0f) * r * len * c.walk_cost + 2.0f + r;   // (one workgroup on a CU: slower)
         if (n > 1)
-            time += rounds((n - 1) * states * c.summaries) * len * c.summary_cost + 3.5f + (n > kMostSegmentsAddedUp ? 6.0f : 0.4f * n);
+            time += rounds((n - 1) * states * c.summaries) * len * c.summary_cost + 3.5f + (n > c.most_added_up ? 6.0f : 0.4f * n);
         if (best_time >= 0.0f && time >= best_time) return;
         best = len;
         best_time = time;
     };
     consider(1);
-    consider(kMostSegmentsAddedUp);
+    consider(c.most_added_up);
     for (int r = 1; r <= c.walks * (int)(kWalkWorkgroups / gka::kComputeUnits); ++r) {
         const int64_t segs = r * gka::kComputeUnits / (states * c.walks);
         if (segs > 1) consider(segs);
@@ -136,17 +145,20 @@ int walk_segment(int64_t states, int64_t chunks, const PassCost &c)
     return (int)best;
 }
 
-// slices: of dv, of the walk whose workgroups the segments are counted for (0: of this one).
-gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv, int slices, const PassCost &cost, WalkPlan *w)
+// like: a walk with the same segments (null: none).
+gka_status plan_walk(const gka_linear_params *p, const Sizes &s, int dk, int dv, const PassCost &cost, const WalkPlan *like, WalkPlan *w)
 {
     w->shape = gka::linear_shape(s.bf16, dk, dv);
     const int64_t chunks = ((int64_t)p->T + w->shape.chunk - 1) / w->shape.chunk;
-    if (p->walk_chunks > 0) w->seg_chunks = p->walk_chunks < chunks ? p->walk_chunks : (int)chunks;
-    else w->seg_chunks = walk_segment(s.pairs * (slices > 0 ? slices : w->shape.slices), chunks, cost);
+    if (like) w->seg_chunks = like->seg_chunks;
+    else if (p->walk_chunks > 0) w->seg_chunks = p->walk_chunks < chunks ? p->walk_chunks : (int)chunks;
+    else w->seg_chunks = walk_segment(s.pairs * w->shape.slices, chunks, cost);
     w->n_segs = (int)((chunks + w->seg_chunks - 1) / w->seg_chunks);
+    w->scanned = w->n_segs > cost.most_added_up;
     const int64_t states = s.pairs * w->shape.slices * w->n_segs;
-    // (three walks of 512 threads are one launch; of the scan, 64 threads for 256 floats, with its 16 segments and more, less)
+    // (three walks of 512 threads are one launch; the scan: a thread for four floats of a state)
     if (states * 3 * 512 >= kGridThreads) return GKA_ERR_SHAPE;
+    if (w->n_segs > 1 && s.pairs * w->shape.slices * (w->shape.state_floats / 4) >= kGridThreads) return GKA_ERR_SHAPE;
     w->state_bytes = w->n_segs > 1 ? align_up((size_t)states * w->shape.state_floats * sizeof(float), 256) : 0;
     w->decay_bytes = w->n_segs > 1 ? align_up((size_t)s.pairs * w->n_segs * sizeof(float), 256) : 0;
     return GKA_OK;
@@ -162,7 +174,7 @@ gka::LinearWalkArgs walk_args(const gka_linear_params *p, const Sizes &s, const 
     a.dk = dk; a.dv = dv;
     a.share = 1;
     a.n_segs = w.n_segs; a.seg_chunks = w.seg_chunks;
-    a.scanned = w.n_segs > kMostSegmentsAddedUp;
+    a.scanned = w.scanned;
     a.slices = w.shape.slices;
     a.seg_states = (float *)ws;
     a.seg_decay = (float *)(ws + w.state_bytes);
@@ -180,9 +192,10 @@ gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
     gka_status e = check(p, Call::kWalk, &b->s);
     if (e != GKA_OK) return e;
     // (the walks of dk and dv have their segments in common)
-    if ((e = plan_walk(p, b->s, p->d_v, p->d_k, 0, backward_cost(b->s.G), &b->q)) != GKA_OK) return e;
+    const PassCost cost = backward_cost(b->s.G, gka::linear_shape(b->s.bf16, p->d_v, p->d_k).state_floats);
+    if ((e = plan_walk(p, b->s, p->d_v, p->d_k, cost, nullptr, &b->q)) != GKA_OK) return e;
     b->k = b->q;
-    if ((e = plan_walk(p, b->s, p->d_k, p->d_v, b->q.shape.slices, backward_cost(b->s.G), &b->v)) != GKA_OK) return e;
+    if ((e = plan_walk(p, b->s, p->d_k, p->d_v, cost, &b->q, &b->v)) != GKA_OK) return e;
     size_t off = 0;
     b->off_q = off; off += b->q.state_bytes + b->q.decay_bytes;
     b->off_k = off; off += b->k.state_bytes + b->k.decay_bytes;
@@ -257,7 +270,7 @@ size_t gka_linear_forward_workspace_bytes(const gka_linear_params *p)
 {
     Sizes s;
     WalkPlan w;
-    if (check(p, Call::kWalk, &s) != GKA_OK || plan_walk(p, s, p->d_k, p->d_v, 0, forward_cost(s.G), &w) != GKA_OK) return 0;
+    if (check(p, Call::kWalk, &s) != GKA_OK || plan_walk(p, s, p->d_k, p->d_v, forward_cost(s.G), nullptr, &w) != GKA_OK) return 0;
     const size_t bytes = w.state_bytes + w.decay_bytes;
     return bytes > 0 ? bytes : 256;
 }
@@ -269,7 +282,7 @@ gka_status gka_linear_forward(const gka_linear_params *p, const void *q, const v
     WalkPlan w;
     gka_status e = check(p, Call::kWalk, &s);
     if (e != GKA_OK) return e;
-    if ((e = plan_walk(p, s, p->d_k, p->d_v, 0, forward_cost(s.G), &w)) != GKA_OK) return e;
+    if ((e = plan_walk(p, s, p->d_k, p->d_v, forward_cost(s.G), nullptr, &w)) != GKA_OK) return e;
     if (!q || !k || !v || !gate || !o) return GKA_ERR_NULL;
     if (misaligned({q, k, v, o, S_init, S_final})) return GKA_ERR_SHAPE;
     if (S_final && S_final == S_init && s.share > 1) return GKA_ERR_SHAPE;   // (states that other sequences still read)
