@@ -17,7 +17,8 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 // A row of the state (one v-feature) lies across LPR lanes, 4 J k-features on each (runs of four, 4 LPR apart); a thread holds NR
 // rows, a workgroup (256 / LPR) NR of them. Few lanes to a row: a token costs each of its G heads a sum over them. The state
 // crosses memory once, whatever the number of tokens. Rows of q, k, v and gates come through LDS, as many tokens at a time as
-// fit, so that their latency is paid once and beside the state's.
+// fit, so that their latency is paid once and beside the state's. Bound by HBM: 8192 states of d 128 in 192 us, 5.6 TB/s (a large copy:
+// 5.3); 384 states of 4 tokens x 4 heads, 16 us, by the sums over a row's lanes.
 constexpr int kDecodeQueries = 32;                 // q rows of a pass through LDS, or those of one token in parts of as many
 constexpr int kDecodeTokens = 16;                  // tokens of a pass at most
 
@@ -124,11 +125,14 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a, 
 // ---- shared ----------------------------------------------------------------------------------------------------------
 // A workgroup takes up to 16 columns of one (prefix, kv head): a column is a query head of a sequence, G of them to a
 // sequence, one behind the other. First S q of its columns on the matrix cores (16 x 16 tiles: 16 rows of S to a wave; S cut into
-// two bf16 pieces, or float32), then each wave the cached tokens of its columns, up to four of one sequence at a time, LR lanes to
-// a row of 16-byte pieces.
+// two bf16 pieces, 16 bits against the 8 of the output, or float32), then each wave the cached tokens of its columns, up to HEADS of
+// one sequence at a time, LR lanes to a row of 16-byte pieces.
+// Bound by the latency of a wave's reads, one batch after the other: 256 samples of 4 prefixes, 32 heads of d 128, up to 128 tokens:
+// 67 us for 262 MiB (4.1 TB/s) from HBM. One head alone leaves registers for 16 reads in flight instead of 8 (72 us). Waves that take the
+// columns by falling length instead of in their order: 1 per cent, not kept.
 constexpr int kSharedCols = 16, kSharedHeads = 4, kSharedWaves = 8;
 
-template <bool BF16, int LR>
+template <bool BF16, int LR, int HEADS>
 __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(LinearSharedArgs a, int ncol)
 {
     typedef std::conditional_t<BF16, IOBF16, IOF32> IO;
@@ -211,7 +215,7 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
         const int b = prefix * a.share + (int)(col / a.G), head0 = (int)(col % a.G);
         int m = a.G - head0;                       // columns of this sequence, taken together
         m = m < c_end - c ? m : c_end - c;
-        m = m < kSharedHeads ? m : kSharedHeads;
+        m = m < HEADS ? m : HEADS;
         const int len = a.lengths[b];
         if (len < 0 || len >= a.N) {               // an idle row of the batch: nothing of it is touched
             c += m;
@@ -227,9 +231,9 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
             if (r == 0 && v_in) *(u32x4_t *)(vc + len * vc_step + E * l) = *(const u32x4_t *)(v_new + E * l);
             if (!a.gate_per_head && lane == 0) a.gate_cache[cache_row + (int64_t)len * a.Hkv] = gate_new;
         }
-        float q[kSharedHeads][E], y[kSharedHeads][E];
+        float q[HEADS][E], y[HEADS][E];
 #pragma unroll
-        for (int i = 0; i < kSharedHeads; ++i) {
+        for (int i = 0; i < HEADS; ++i) {
             const elem_t *row = row_of(a.q, b, h * a.G + head0 + (i < m ? i : 0));
 #pragma unroll
             for (int e = 0; e < E; ++e) y[i][e] = 0.0f;
@@ -254,7 +258,7 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
                 for (int e = 0; e < 4; ++e) x[e] = u[e];
             }
         };
-        constexpr int FLY = LR < 8 ? LR : 8;       // reads in flight
+        constexpr int MOST = HEADS == 1 ? 16 : 8, FLY = LR < MOST ? LR : MOST;    // reads in flight
         double behind = 0.0;                       // log2 decay over the tokens behind the tile
         for (int j0 = len / 64 * 64; j0 >= 0; j0 -= 64) {
             const int count = len + 1 - j0 < 64 ? len + 1 - j0 : 64;
@@ -272,7 +276,7 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
                     float x[E];
                     floats(p[i], x);
 #pragma unroll
-                    for (int g = 0; g < kSharedHeads; ++g) {
+                    for (int g = 0; g < HEADS; ++g) {
                         if (g < m) {
                             float dot = 0.0f;
 #pragma unroll
@@ -288,7 +292,7 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
             behind += total;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the wave's own scores)
 #pragma unroll
-            for (int g = 0; g < kSharedHeads; ++g)
+            for (int g = 0; g < HEADS; ++g)
                 if (g < m) score[g * 64 + lane] = lane < count ? score[g * 64 + lane] * weight : 0.0f;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             for (int s0 = 0; s0 < count; s0 += FLY * RP) {
@@ -300,7 +304,7 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
                     float x[E];
                     floats(p[i], x);
 #pragma unroll
-                    for (int g = 0; g < kSharedHeads; ++g) {
+                    for (int g = 0; g < HEADS; ++g) {
                         if (g < m) {
                             const float s = score[g * 64 + s0 + i * RP + r];
 #pragma unroll
@@ -313,7 +317,7 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
         }
         const float zeta = __builtin_amdgcn_exp2f((float)behind);
 #pragma unroll
-        for (int g = 0; g < kSharedHeads; ++g) {
+        for (int g = 0; g < HEADS; ++g) {
             if (g >= m) continue;
 #pragma unroll
             for (int e = 0; e < E; ++e)
@@ -381,19 +385,25 @@ hipError_t launch_decode(const LinearDecodeArgs &a, hipStream_t stream)
     return launch_decode_dk<BF16, 256>(a, stream);
 }
 
-template <bool BF16, int LR>
-hipError_t launch_shared(const LinearSharedArgs &a, hipStream_t stream)
+template <bool BF16, int LR, int HEADS>
+hipError_t launch_shared_heads(const LinearSharedArgs &a, hipStream_t stream)
 {
     const int64_t cols = (int64_t)a.share * a.G, groups = (int64_t)(a.B / a.share) * a.Hkv;
-    // two workgroups to a CU, with fewer columns to each where there are not so many (four: 75 us instead of 63 for 64 samples of 4
+    // two workgroups to a CU, with fewer columns to each where there are not so many (four instead: 75 us against 63, 64 samples of 4
     // prefixes, 32 heads)
     int ncol = kSharedCols;
     while (ncol > 1 && groups * ((cols + ncol - 1) / ncol) < 512) ncol /= 2;
     const int64_t blocks = groups * ((cols + ncol - 1) / ncol);
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     const size_t lds = ((size_t)ncol * (a.dv + 4) + kSharedWaves * kSharedHeads * 64) * sizeof(float);
-    hipLaunchKernelGGL((linear_shared_kernel<BF16, LR>), dim3((unsigned)blocks), dim3(64 * kSharedWaves), lds, stream, a, ncol);
+    hipLaunchKernelGGL((linear_shared_kernel<BF16, LR, HEADS>), dim3((unsigned)blocks), dim3(64 * kSharedWaves), lds, stream, a, ncol);
     return hipGetLastError();
+}
+
+template <bool BF16, int LR>
+hipError_t launch_shared(const LinearSharedArgs &a, hipStream_t stream)
+{
+    return a.G == 1 ? launch_shared_heads<BF16, LR, 1>(a, stream) : launch_shared_heads<BF16, LR, kSharedHeads>(a, stream);
 }
 
 template <bool BF16>
