@@ -417,6 +417,18 @@ __device__ __forceinline__ float sum_over_kg(float x)
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+__device__ __forceinline__ double sum_over_kg_f64(double x)
+{
+    const uint32_t lo = (uint32_t)__double2loint(x), hi = (uint32_t)__double2hiint(x);
+    const auto l0 = __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+    const auto h0 = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+    x = __hiloint2double((int)h0[0], (int)l0[0]) + __hiloint2double((int)h0[1], (int)l0[1]);
+    const uint32_t lo2 = (uint32_t)__double2loint(x), hi2 = (uint32_t)__double2hiint(x);
+    const auto l1 = __builtin_amdgcn_permlane32_swap(lo2, lo2, false, false);
+    const auto h1 = __builtin_amdgcn_permlane32_swap(hi2, hi2, false, false);
+    return __hiloint2double((int)h1[0], (int)l1[0]) + __hiloint2double((int)h1[1], (int)l1[1]);
+}
+
 // Sum over aligned groups of N lanes (a power of two), to all of them, by vector moves.
 template <int N>
 __device__ __forceinline__ float sum_over_lanes(float x)

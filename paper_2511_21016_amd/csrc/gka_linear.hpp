@@ -32,9 +32,9 @@ struct LinearWalkArgs {
     int final_times_gate;         // ... times the gate of the tensors' token 0 (the gradient at the initial state)
     // what the gradient of the decays is made of (written where the pointers are not null, in the order [slices, B, H_kv, ...]):
     RowTensor dot_with;           // like y: dot_out [slices, B, H_kv, n_q, T] = dot_with . y, y before it is rounded
-    float *dot_out;
+    double *dot_out;
     const float *state_dot_with;  // [B, H_kv, dv, dk]: state_dot_out [slices, B, H_kv] = its product with the last state
-    float *state_dot_out;
+    double *state_dot_out;
     // plan
     int n_segs, seg_chunks;       // segments of the walk, chunks each
     int scanned;                  // a launch between turns what the segments add into the states that they start from (else each
@@ -78,9 +78,9 @@ hipError_t launch_linear_backward_f32_256(const LinearWalkArgs &dq, const Linear
 
 // dgate_t = ([state_dot] + sum_{s >= t} (q . dq - k . dk)) / gate_t, and the sum of gradients at shared initial states.
 struct LinearGateArgs {
-    const float *q_dq;            // [q_slices, B, H_kv, G, T]
-    const float *k_dk;            // [k_slices, B, H_kv, T]
-    const float *state_dot;       // [q_slices, B, H_kv] or nullptr
+    const double *q_dq;           // [q_slices, B, H_kv, G, T]
+    const double *k_dk;           // [k_slices, B, H_kv, T]
+    const double *state_dot;      // [q_slices, B, H_kv] or nullptr
     int q_slices, k_slices, G;
     const float *gate;
     float *dgate;                 // [B, T, H_kv], or [H_kv] with gate_per_head

@@ -203,9 +203,9 @@ gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
     if (b->s.pairs * ((p->T + (int64_t)4095) / 4096) * 1024 >= kGridThreads || b->s.pairs * p->d_k * p->d_v / 4 >= kGridThreads)
         return GKA_ERR_SHAPE;
     const size_t tokens = (size_t)b->s.pairs * p->T;
-    b->off_q_dot = off; off += align_up(b->q.shape.slices * tokens * b->s.G * sizeof(float), 256);
-    b->off_k_dot = off; off += align_up(b->k.shape.slices * tokens * sizeof(float), 256);
-    b->off_state_dot = off; off += align_up(b->q.shape.slices * b->s.pairs * sizeof(float), 256);
+    b->off_q_dot = off; off += align_up(b->q.shape.slices * tokens * b->s.G * sizeof(double), 256);
+    b->off_k_dot = off; off += align_up(b->k.shape.slices * tokens * sizeof(double), 256);
+    b->off_state_dot = off; off += align_up(b->q.shape.slices * b->s.pairs * sizeof(double), 256);
     b->off_gate = off; off += align_up(gka::linear_gate_workspace_bytes(b->s.pairs, p->T), 256);
     b->off_states = off;
     // (room for a state of every sequence whether or not initial states are shared: one size for all calls)
@@ -318,7 +318,7 @@ gka_status gka_linear_backward(const gka_linear_params *p, const void *q, const 
     hipStream_t stream = (hipStream_t)hip_stream;
     char *ws = (char *)workspace;
     const Sizes &s = b.s;
-    float *q_dot = (float *)(ws + b.off_q_dot), *k_dot = (float *)(ws + b.off_k_dot), *state_dot = (float *)(ws + b.off_state_dot);
+    double *q_dot = (double *)(ws + b.off_q_dot), *k_dot = (double *)(ws + b.off_k_dot), *state_dot = (double *)(ws + b.off_state_dot);
     const int64_t none[3] = {0, 0, 0};
     gka::RowTensor packed_q, packed_k, packed_v;
     (void)row_strides(none, p, p->T, p->H, p->d_k, &packed_q);

@@ -11,7 +11,7 @@ namespace {
 // A gate of at most exp(-100) wipes the state (L_t = 0 there): the sum starts anew before it and its own gradient is
 // written as 0. A workgroup takes up to 4096 tokens of a (sequence, kv head), four consecutive ones to a thread, joined by a scan over
 // the threads in float64; of longer sequences a first launch (SUMS) leaves what each part adds up to. 64 heads x 4096 tokens: 13 us for
-// 4 MiB, bound by the latency of one chain (gates and results of a head lie H_kv apart).
+// 6 MiB, bound by the latency of one chain (gates and results of a head lie H_kv apart).
 constexpr int kThreads = 1024, kRun = 4, kPart = kThreads * kRun;
 constexpr float kWiped = 3.8e-44f;                 // exp(-100) to float32's last bits there
 
@@ -39,10 +39,10 @@ __global__ __launch_bounds__(kThreads) void linear_gate_kernel(LinearGateArgs a)
     for (int s = 0; s < a.q_slices; ++s)
         for (int g = 0; g < a.G; ++g)
 #pragma unroll
-            for (int i = 0; i < kRun; ++i) x[i] += (double)a.q_dq[(((int64_t)s * n_pairs + pair) * a.G + g) * a.T + at[i]];
+            for (int i = 0; i < kRun; ++i) x[i] += a.q_dq[(((int64_t)s * n_pairs + pair) * a.G + g) * a.T + at[i]];
     for (int s = 0; s < a.k_slices; ++s)
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) x[i] -= (double)a.k_dk[((int64_t)s * n_pairs + pair) * a.T + at[i]];
+        for (int i = 0; i < kRun; ++i) x[i] -= a.k_dk[((int64_t)s * n_pairs + pair) * a.T + at[i]];
 #pragma unroll
     for (int i = 0; i < kRun; ++i)
         if (t0 + i >= a.T) {
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kThreads) void linear_gate_kernel(LinearGateArgs a)
     // what comes from behind this wave
     double c = 0.0;
     if (a.state_dot)
-        for (int s = 0; s < a.q_slices; ++s) c += (double)a.state_dot[(int64_t)s * n_pairs + pair];
+        for (int s = 0; s < a.q_slices; ++s) c += a.state_dot[(int64_t)s * n_pairs + pair];
     for (int i = parts - 1; i > part; --i) {
         const int64_t at = (int64_t)pair * parts + i;
         c = a.part_sums[at] + (a.part_open[at] ? c : 0.0);

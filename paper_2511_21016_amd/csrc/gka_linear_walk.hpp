@@ -260,7 +260,7 @@ struct Shape {
     static constexpr size_t q_bytes = (size_t)C * QT::ROW, k_bytes = (size_t)C * KT::ROW, v_bytes = (size_t)C * VT::ROW;
     static constexpr size_t unit_bytes = M::STEPS * 64 * sizeof(typename M::frag);
     static constexpr size_t tables = 2 * 5 * 64 * sizeof(float);
-    static constexpr size_t dot_bytes = (size_t)NW * C * sizeof(float);
+    static constexpr size_t dot_bytes = (size_t)NW * C * sizeof(double);
     static constexpr size_t p_bytes(int pieces) { return UNITS * unit_bytes * pieces; }
     static constexpr size_t lds_bytes(int pieces, bool summary, bool dot)
     {
@@ -424,7 +424,7 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     unsigned char *sK = smem, *sV = smem + SH::k_bytes;
     float *tables = (float *)(sV + SH::v_bytes);   // [2][5][64]: log2 decay (two floats), weight in the state, zeta of a token (both with the state's factor); that factor
     unsigned char *sQ = (unsigned char *)tables + SH::tables, *sP = sQ + SH::q_bytes;
-    float *sDot = (float *)(sP + SH::p_bytes(PIECES));         // [NW][C]: the waves' parts of the dot products (DOT)
+    double *sDot = (double *)(sP + SH::p_bytes(PIECES));        // [NW][C]: the waves' parts of the dot products (DOT)
 
     const int tid = threadIdx.x;
     const int lane0 = tid & 63, lane = lane0;
@@ -576,7 +576,7 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     auto add_dots = [&](int c, int s) {
         const int lane = anew(lane0), tau = c * C + lane;
         if (w != NW - 2 || lane >= C || tau >= a.T) return;
-        float dot = 0.0f;
+        double dot = 0.0;
 #pragma unroll
         for (int i = 0; i < NW; ++i) dot += sDot[i * C + lane];
         a.dot_out[(((int64_t)slice * n_pairs + pair) * a.n_q + s) * a.T + (a.reverse ? a.T - 1 - tau : tau)] = dot;
@@ -779,10 +779,10 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                             f32x4 x;
                             if constexpr (BF16) x = IOBF16::cvt4(__builtin_bit_cast(u16x4, dot_row[tb]));
                             else x = __builtin_bit_cast(f32x4, dot_row[tb]);
-                            float dot = 0.0f;
+                            double dot = 0.0;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) dot += x[e] * y[tb][e];
-                            dot = sum_over_kg(dot);
+                            for (int e = 0; e < 4; ++e) dot += (double)x[e] * (double)y[tb][e];
+                            dot = sum_over_kg_f64(dot);
                             if (kg == 0) sDot[w * C + 16 * tb + n] = dot;
                         }
                     }
@@ -882,21 +882,21 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     } else if (seg == a.n_segs - 1) {
         if (a.state_dot_out) {
             const StateAt S(a.state_dot_with, pair, a, v0 + 16 * w, lane);
-            float dot = 0.0f;
+            double dot = 0.0;
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 const f32x4 x = S.load(j);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) dot += x[e] * acc[j][e];
+                for (int e = 0; e < 4; ++e) dot += (double)x[e] * (double)acc[j][e];
             }
-            dot = wave_sum(dot);
+            dot = lane63_f64(wave_inclusive_scan_f64(dot));
             lds_barrier();
-            if (lane == 0) tables[w] = dot;
+            if (lane == 0) ((double *)tables)[w] = dot;
             lds_barrier();
             if (tid == 0) {
-                float all = 0.0f;
+                double all = 0.0;
 #pragma unroll
-                for (int i = 0; i < NW; ++i) all += tables[i];
+                for (int i = 0; i < NW; ++i) all += ((const double *)tables)[i];
                 a.state_dot_out[(int64_t)slice * n_pairs + pair] = all;
             }
         }
