@@ -98,6 +98,13 @@ def test_shared_in_bulk():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_shared_in_bulk_of_one_query_head_with_idle_rows(dtype):
+    lengths = np.random.default_rng(4).integers(-3, 24, 2200)
+    args = shared_inputs(2, 1100, 20, 4, 4, 64, 64, dtype, False, lengths)
+    check_shared(args, torch.full((2200, 4, 64), 3.0, dtype=args[1].dtype, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_shared_idle_rows_full_caches_and_borders(dtype):
     args = shared_inputs(2, 6, 129, 4, 2, 64, 64, dtype, False, [-1, 0, 1, 62, 63, 64, 65, 127, 128, 129, 2 ** 31 - 1, -2 ** 31])
     check_shared(args, torch.full((12, 4, 64), 3.0, dtype=args[1].dtype, device="cuda"))
