@@ -372,7 +372,8 @@ typedef struct {
     int32_t reserved;     /* 0 (GKA_ERR_UNSUPPORTED)                                                   */
     int64_t q_stride[3];  /* element strides of batch, token and head (the features of a row are       */
     int64_t k_stride[3];  /*   contiguous): positive, multiples of 16 bytes, a row or more from head   */
-    int64_t v_stride[3];  /*   to head and token to token, below 2^23 from token to token; 0,0,0 = packed */
+    int64_t v_stride[3];  /*   to head and token to token (of one token not used), below 2^23 from token  */
+                          /*   to token in gka_linear_forward and _backward; 0,0,0 = packed            */
     int64_t o_stride[3];  /* of o, and of dy in the backward pass                                      */
 } gka_linear_params;
 

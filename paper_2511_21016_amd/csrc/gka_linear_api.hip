@@ -36,24 +36,27 @@ struct Sizes {
 
 enum class Call { kWalk, kDecode, kShared };
 
-// Strides of one tensor [B, T, heads, d]; all zero: packed.
-gka_status row_strides(const int64_t (&given)[3], const gka_linear_params *p, int T, int heads, int d, gka::RowTensor *x)
+// Strides of one tensor [B, T, heads, d]; all zero: packed. The walks address a chunk's rows with 32-bit byte offsets; the calls for
+// single tokens use 64 bits, and of one token the stride to the next is not used at all.
+gka_status row_strides(const int64_t (&given)[3], const gka_linear_params *p, Call call, int T, int heads, int d, gka::RowTensor *x)
 {
+    constexpr int64_t kChunkRows = 1 << 23;
+    const bool chunks = call == Call::kWalk && T > 1;
     x->p = nullptr;
     x->sh = d;
     x->st = (int64_t)heads * d;
     x->sb = (int64_t)T * heads * d;
-    if (x->st >= 1 << 23) return GKA_ERR_UNSUPPORTED;
-    if (given[0] == 0 && given[1] == 0 && given[2] == 0) return GKA_OK;
-    const int piece = p->io_dtype == GKA_BF16 ? 8 : 4;            // rows are read and written 16 bytes at a time
-    for (int64_t s : given)
-        if (s <= 0 || s % piece) return GKA_ERR_SHAPE;
-    if ((heads > 1 && given[2] < d) || given[1] < d) return GKA_ERR_SHAPE;
-    if (given[1] >= 1 << 23) return GKA_ERR_UNSUPPORTED;          // (a chunk's rows are addressed with 32-bit byte offsets)
-    x->sb = given[0];
-    x->st = given[1];
-    x->sh = given[2];
-    return GKA_OK;
+    if (given[0] != 0 || given[1] != 0 || given[2] != 0) {
+        const int piece = p->io_dtype == GKA_BF16 ? 8 : 4;        // rows are read and written 16 bytes at a time
+        for (int64_t s : given)
+            if (s <= 0 || s % piece) return GKA_ERR_SHAPE;
+        if ((heads > 1 && given[2] < d) || (T > 1 && given[1] < d)) return GKA_ERR_SHAPE;
+        x->sb = given[0];
+        x->st = given[1];
+        x->sh = given[2];
+    }
+    if (T == 1) x->st = d;
+    return chunks && x->st >= kChunkRows ? GKA_ERR_UNSUPPORTED : GKA_OK;
 }
 
 gka_status check(const gka_linear_params *p, Call call, Sizes *s)
@@ -76,10 +79,10 @@ gka_status check(const gka_linear_params *p, Call call, Sizes *s)
     // (of decode up to eight workgroups of 256 threads for a state where there are this many, of the shared call one of 512 for 16 heads)
     if (s->pairs >= (int64_t)1 << 21 || (int64_t)p->B * p->H > (int64_t)1 << 26) return GKA_ERR_SHAPE;
     const int T = call == Call::kShared ? 1 : p->T;
-    gka_status e = row_strides(p->q_stride, p, T, p->H, p->d_k, &s->q);
-    if (e == GKA_OK) e = row_strides(p->k_stride, p, T, p->H_kv, p->d_k, &s->k);
-    if (e == GKA_OK) e = row_strides(p->v_stride, p, T, p->H_kv, p->d_v, &s->v);
-    if (e == GKA_OK) e = row_strides(p->o_stride, p, T, p->H, p->d_v, &s->o);
+    gka_status e = row_strides(p->q_stride, p, call, T, p->H, p->d_k, &s->q);
+    if (e == GKA_OK) e = row_strides(p->k_stride, p, call, T, p->H_kv, p->d_k, &s->k);
+    if (e == GKA_OK) e = row_strides(p->v_stride, p, call, T, p->H_kv, p->d_v, &s->v);
+    if (e == GKA_OK) e = row_strides(p->o_stride, p, call, T, p->H, p->d_v, &s->o);
     return e;
 }
 
@@ -321,9 +324,9 @@ gka_status gka_linear_backward(const gka_linear_params *p, const void *q, const 
     double *q_dot = (double *)(ws + b.off_q_dot), *k_dot = (double *)(ws + b.off_k_dot), *state_dot = (double *)(ws + b.off_state_dot);
     const int64_t none[3] = {0, 0, 0};
     gka::RowTensor packed_q, packed_k, packed_v;
-    (void)row_strides(none, p, p->T, p->H, p->d_k, &packed_q);
-    (void)row_strides(none, p, p->T, p->H_kv, p->d_k, &packed_k);
-    (void)row_strides(none, p, p->T, p->H_kv, p->d_v, &packed_v);
+    (void)row_strides(none, p, Call::kWalk, p->T, p->H, p->d_k, &packed_q);
+    (void)row_strides(none, p, Call::kWalk, p->T, p->H_kv, p->d_k, &packed_k);
+    (void)row_strides(none, p, Call::kWalk, p->T, p->H_kv, p->d_v, &packed_v);
     // dq_t = S_t^T dy_t
     gka::LinearWalkArgs wq = walk_args(p, s, b.q, gate, p->d_v, p->d_k, ws + b.off_q);
     wq.q = at(dy, s.o); wq.k = at(v, s.v); wq.v = at(k, s.k); wq.y = at(dq, packed_q);
