@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a, 
 // ---- shared ----------------------------------------------------------------------------------------------------------
 // A workgroup takes up to 16 columns of one (prefix, kv head): a column is a query head of a sequence, G of them to a
 // sequence, one behind the other. First S q of its columns on the matrix cores (16 x 16 tiles: 16 rows of S to a wave; S cut into
-// two bf16 pieces, 16 bits against the 8 of the output, or float32), then each wave the cached tokens of its columns, up to HEADS of
+// three bf16 pieces, which hold all its bits, or float32), then each wave the cached tokens of its columns, up to HEADS of
 // one sequence at a time, LR lanes to a row of 16-byte pieces.
 // Bound by the latency of a wave's reads, one batch after the other: 256 samples of 4 prefixes, 32 heads of d 128, up to 128 tokens:
 // 67 us for 262 MiB (4.1 TB/s) from HBM. One head alone leaves registers for 16 reads in flight instead of 8 (72 us). Waves that take the
@@ -183,12 +183,15 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
                 for (int i = 0; i < FLY; ++i) {
                     if constexpr (BF16) {
                         float x[8] = {x0[i][0], x0[i][1], x0[i][2], x0[i][3], x1[i][0], x1[i][1], x1[i][2], x1[i][3]}, back[8];
-                        const bf16x8 hi = MmaBF16::pack(x), qf = __builtin_bit_cast(bf16x8, q0[i]);
-                        MmaBF16::unpack(hi, back);
+                        const bf16x8 qf = __builtin_bit_cast(bf16x8, q0[i]);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] -= back[e];
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, qf, acc, 0, 0, 0);
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(MmaBF16::pack(x), qf, acc, 0, 0, 0);
+                        for (int piece = 0; piece < 3; ++piece) {
+                            const bf16x8 f = MmaBF16::pack(x);
+                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf, acc, 0, 0, 0);
+                            MmaBF16::unpack(f, back);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] -= back[e];
+                        }
                     } else {
                         const f32x4 qa = __builtin_bit_cast(f32x4, q0[i]), qb = __builtin_bit_cast(f32x4, q1[i]);
 #pragma unroll

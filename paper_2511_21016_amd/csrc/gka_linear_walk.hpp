@@ -20,10 +20,10 @@
 // 32 features a wave would need 256 registers, two waves on a SIMD.
 //
 // Precision. bf16 tensors enter the products as they are; what is computed in float32 (states, masked products, weighted
-// v) is cut into bf16 pieces of 8 bits each: two where the product ends in a bf16 output (17 bits against the output's 8), three
-// where it ends in float32: in a state that is asked for, and in the dot products behind the gradient of the decays, a long sum
-// of differences. float32 tensors use the float32 MFMA. Decays are summed in float64 and kept as two floats: a difference of
-// two of them is then exact to float32 wherever a sequence is wiped by a gate of 0 (2^-144 each) before.
+// v) is cut into three bf16 pieces, which hold all of its 24 bits. (Two pieces in the readout round one in 400 of the bf16 outputs
+// the other way than its exact value, and take 13 per cent less: 64 states of d 128 x 4096 tokens, 107 us the pass against 120.)
+// float32 tensors use the float32 MFMA. Decays are summed in float64 and kept as two floats: a difference of two of them is then
+// exact to float32 wherever a sequence is wiped by a gate of 0 (2^-144 each) before.
 #pragma once
 #include "gka_device.hpp"
 #include "gka_linear.hpp"
@@ -37,7 +37,7 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 // Products of 16 x 16 tiles. STEPS: MFMAs for a contraction over 32; VEC: operand elements per lane of each.
 struct Tile16BF16 {
     static constexpr bool BF16 = true;
-    static constexpr int VEC = 8, STEPS = 1;
+    static constexpr int VEC = 8, STEPS = 1, PIECES = 3;       // (of a float32 operand)
     typedef bf16x8 frag;
     typedef uint16_t elem_t;
     static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -46,7 +46,7 @@ struct Tile16BF16 {
 };
 struct Tile16F32 {
     static constexpr bool BF16 = false;
-    static constexpr int VEC = 1, STEPS = 8;
+    static constexpr int VEC = 1, STEPS = 8, PIECES = 1;
     typedef float frag;
     typedef float elem_t;
     static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
@@ -261,10 +261,10 @@ struct Shape {
     static constexpr size_t unit_bytes = M::STEPS * 64 * sizeof(typename M::frag);
     static constexpr size_t tables = 2 * 5 * 64 * sizeof(float);
     static constexpr size_t dot_bytes = (size_t)NW * C * sizeof(double);
-    static constexpr size_t p_bytes(int pieces) { return UNITS * unit_bytes * pieces; }
-    static constexpr size_t lds_bytes(int pieces, bool summary, bool dot)
+    static constexpr size_t p_bytes = UNITS * unit_bytes * M::PIECES;
+    static constexpr size_t lds_bytes(bool summary, bool dot)
     {
-        return k_bytes + v_bytes + tables + (summary ? 0 : q_bytes + p_bytes(pieces) + (dot ? dot_bytes : 0));
+        return k_bytes + v_bytes + tables + (summary ? 0 : q_bytes + p_bytes + (dot ? dot_bytes : 0));
     }
     static_assert((C * DK / E) % NT == 0 && NT % (DK / E) == 0, "a thread's pieces lie in one column");
 };
@@ -405,9 +405,8 @@ enum Group { kOne, kQueries, kSources };           // n_q = n_src = 1; several q
 // Waves on a SIMD that a kernel's registers are limited for: two workgroups of a CU's LDS, one with 256 k-features.
 constexpr int walk_waves(int dk, int nw) { return nw == 8 && dk <= 128 ? 4 : 2; }
 
-// PIECES: of states and masked products in the readout, VW: of the weighted v (float32 tensors: 1). DOT: dot_out is wanted.
-// TURNED: see SegStates.
-template <class M, int DK, int NW, int PIECES, int VW, bool DOT, bool SUMMARY, Group GROUP, bool TURNED = false>
+// DOT: dot_out is wanted. TURNED: see SegStates.
+template <class M, int DK, int NW, bool DOT, bool SUMMARY, Group GROUP, bool TURNED = false>
 __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
 {
     typedef Shape<M, DK, NW> SH;
@@ -417,14 +416,14 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     typedef typename M::frag frag;
     constexpr bool BF16 = M::BF16;
     constexpr int C = SH::C, TB = SH::TB, SB = SH::SB, NT = SH::NT, NJ = SH::NJ, KB = SH::KB, E = SH::E, ES = SH::ES, PK = SH::PK,
-                  PV = SH::PV, STEPS = M::STEPS, VEC = M::VEC;
+                  PV = SH::PV, STEPS = M::STEPS, VEC = M::VEC, PIECES = M::PIECES;
     constexpr bool ROOMY = walk_waves(DK, NW) == 2;
     constexpr int LOOKAHEAD = ROOMY ? 4 : GROUP == kSources ? 1 : 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char *sK = smem, *sV = smem + SH::k_bytes;
     float *tables = (float *)(sV + SH::v_bytes);   // [2][5][64]: log2 decay (two floats), weight in the state, zeta of a token (both with the state's factor); that factor
     unsigned char *sQ = (unsigned char *)tables + SH::tables, *sP = sQ + SH::q_bytes;
-    double *sDot = (double *)(sP + SH::p_bytes(PIECES));        // [NW][C]: the waves' parts of the dot products (DOT)
+    double *sDot = (double *)(sP + SH::p_bytes);        // [NW][C]: the waves' parts of the dot products (DOT)
 
     const int tid = threadIdx.x;
     const int lane0 = tid & 63, lane = lane0;
@@ -646,15 +645,13 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                                 x[1] = M::mma(kf[1][kb][st], qf[kb][st], k0 + kb + st == 0 ? zero : x[1]);
                             }
                     }
-                    // register r: key 32 sb + 16 half + 4 kg + r, token 16 tb + n. (Where an output is bf16, the second float of the decays is
-                    // left out: it is below 2^-18 unless the chunk holds wiped states, 2^-11 with a wiped one at every token.)
+                    // register r: key 32 sb + 16 half + 4 kg + r, token 16 tb + n
                     const float hi = sHi[16 * tb + n], lo = sLo[16 * tb + n];
                     float m[8];
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int s0 = 32 * sb + 16 * half + 4 * kg, below = tb - 2 * sb - half;
-                        f32x4 d = hi - *(const f32x4 *)(sHi + s0);
-                        if constexpr (!BF16 || PIECES > 2) d += lo - *(const f32x4 *)(sLo + s0);
+                        const f32x4 d = (hi - *(const f32x4 *)(sHi + s0)) + (lo - *(const f32x4 *)(sLo + s0));
                         // (keys behind the token are left out by a selection: they may hold anything)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
@@ -830,7 +827,7 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                 struct Keys {
                     frag f[BATCH];
                 };
-                frag f[VW];
+                frag f[PIECES];
                 in_flight<SB * STEPS * PARTS, Keys>(
                     [&](auto i, Keys &k) {
                         constexpr int part = i % PARTS, st = i / PARTS % STEPS, sb = i / PARTS / STEPS;
@@ -852,10 +849,10 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                             } else {
                                 x[0] *= sW[32 * sb + 16 * (st >> 2) + 4 * kg + (st & 3)];
                             }
-                            cut<M, VW>(x, f);
+                            cut<M, PIECES>(x, f);
                         }
 #pragma unroll
-                        for (int n_piece = 0; n_piece < VW; ++n_piece)
+                        for (int n_piece = 0; n_piece < PIECES; ++n_piece)
 #pragma unroll
                             for (int e = 0; e < BATCH; ++e) acc[part * BATCH + e] = M::mma(k.f[e], f[n_piece], acc[part * BATCH + e]);
                     });
@@ -910,11 +907,11 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     }
 }
 
-template <class M, int DK, int NW, int PIECES, int VW, bool SUMMARY, Group GROUP, bool TURNED>
+template <class M, int DK, int NW, bool SUMMARY, Group GROUP, bool TURNED>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(walk_waves(DK, NW), walk_waves(DK, NW))))
 void linear_walk_kernel(LinearWalkArgs a)
 {
-    walk<M, DK, NW, PIECES, VW, false, SUMMARY, GROUP, TURNED>(a, blockIdx.x);
+    walk<M, DK, NW, false, SUMMARY, GROUP, TURNED>(a, blockIdx.x);
 }
 
 // The walks of the backward pass in one launch, `walks` of them (dq, dk, dv; SUMMARY: dq, dk), groups of eight workgroups of each in
@@ -928,13 +925,12 @@ template <class M, int DK, int NW, bool SUMMARY, bool GROUPED, int WALKS>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(walk_waves(DK, NW), walk_waves(DK, NW))))
 void linear_backward_kernel(LinearBackwardArgs a)
 {
-    constexpr int EXACT = M::BF16 ? 3 : 1, PLAIN = M::BF16 ? 2 : 1;
     const int role = blockIdx.x / 8 % WALKS, workgroup = blockIdx.x / (8 * WALKS) * 8 + blockIdx.x % 8;
     if (workgroup >= a.workgroups) return;
-    if (!GROUPED && role <= 1) walk<M, DK, NW, SUMMARY ? 1 : EXACT, EXACT, !SUMMARY, SUMMARY, kOne>(a.walk[role], workgroup);
-    else if (role == 0) walk<M, DK, NW, SUMMARY ? 1 : EXACT, EXACT, !SUMMARY, SUMMARY, GROUPED && !SUMMARY ? kQueries : kOne>(a.walk[0], workgroup);
-    else if (role == 1) walk<M, DK, NW, SUMMARY ? 1 : EXACT, EXACT, !SUMMARY, SUMMARY, GROUPED ? kSources : kOne>(a.walk[1], workgroup);
-    else if constexpr (WALKS == 3) walk<M, DK, NW, PLAIN, EXACT, false, false, GROUPED ? kSources : kOne, true>(a.walk[2], workgroup);
+    if (!GROUPED && role <= 1) walk<M, DK, NW, !SUMMARY, SUMMARY, kOne>(a.walk[role], workgroup);
+    else if (role == 0) walk<M, DK, NW, !SUMMARY, SUMMARY, GROUPED && !SUMMARY ? kQueries : kOne>(a.walk[0], workgroup);
+    else if (role == 1) walk<M, DK, NW, !SUMMARY, SUMMARY, GROUPED ? kSources : kOne>(a.walk[1], workgroup);
+    else if constexpr (WALKS == 3) walk<M, DK, NW, false, false, GROUPED ? kSources : kOne, true>(a.walk[2], workgroup);
 }
 
 // What the segments add -> the states that they start from, in place, of walk blockIdx.y: a thread carries four floats of a state over
@@ -983,14 +979,14 @@ hipError_t launch_kernel(Kernel kernel, bool (&raised)[kMaxLdsDevices], int work
     return hipGetLastError();
 }
 
-template <class M, int DK, int NW, int PIECES, int VW, bool SUMMARY, Group GROUP, bool TURNED = false>
+template <class M, int DK, int NW, bool SUMMARY, Group GROUP, bool TURNED = false>
 hipError_t launch_one(const LinearWalkArgs &a, hipStream_t stream)
 {
     typedef Shape<M, DK, NW> SH;
-    static_assert(SH::lds_bytes(3, false, true) <= (size_t)160 << 10, "LDS of a CU");
+    static_assert(SH::lds_bytes(false, true) <= (size_t)160 << 10, "LDS of a CU");
     static bool raised[kMaxLdsDevices] = {};
-    return launch_kernel(linear_walk_kernel<M, DK, NW, PIECES, VW, SUMMARY, GROUP, TURNED>, raised,
-                         a.B * a.Hkv * a.slices * (SUMMARY ? a.n_segs - 1 : a.n_segs), SH::NT, SH::lds_bytes(PIECES, SUMMARY, false), a, stream);
+    return launch_kernel(linear_walk_kernel<M, DK, NW, SUMMARY, GROUP, TURNED>, raised,
+                         a.B * a.Hkv * a.slices * (SUMMARY ? a.n_segs - 1 : a.n_segs), SH::NT, SH::lds_bytes(SUMMARY, false), a, stream);
 }
 
 template <int DK, int NW>
@@ -1001,22 +997,16 @@ hipError_t launch_scan(const LinearBackwardArgs &walks, int n, hipStream_t strea
     return hipGetLastError();
 }
 
-// The forward pass. VW: pieces of the weighted v.
-template <class M, int DK, int NW, Group GROUP, int VW>
-hipError_t launch_forward_vw(const LinearWalkArgs &a, hipStream_t stream)
-{
-    if (a.n_segs > 1) {
-        hipError_t e = launch_one<M, DK, NW, 1, VW, true, kOne>(a, stream);
-        if (e == hipSuccess && a.scanned) e = launch_scan<DK, NW>({{a}, 0}, 1, stream);
-        if (e != hipSuccess) return e;
-    }
-    return launch_one<M, DK, NW, M::BF16 ? 2 : 1, VW, false, GROUP>(a, stream);
-}
+// The forward pass.
 template <class M, int DK, int NW, Group GROUP>
 hipError_t launch_forward(const LinearWalkArgs &a, hipStream_t stream)
 {
-    if constexpr (M::BF16) return a.final ? launch_forward_vw<M, DK, NW, GROUP, 3>(a, stream) : launch_forward_vw<M, DK, NW, GROUP, 2>(a, stream);
-    else return launch_forward_vw<M, DK, NW, GROUP, 1>(a, stream);
+    if (a.n_segs > 1) {
+        hipError_t e = launch_one<M, DK, NW, true, kOne>(a, stream);
+        if (e == hipSuccess && a.scanned) e = launch_scan<DK, NW>({{a}, 0}, 1, stream);
+        if (e != hipSuccess) return e;
+    }
+    return launch_one<M, DK, NW, false, GROUP>(a, stream);
 }
 template <class M, int DK>
 hipError_t launch_forward_dk(const LinearWalkArgs &a, hipStream_t stream)
@@ -1032,7 +1022,6 @@ template <class M, int DK, int NW, bool GROUPED>
 hipError_t launch_backward(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream)
 {
     typedef Shape<M, DK, NW> SH;
-    constexpr int PIECES = M::BF16 ? 3 : 1;
     LinearBackwardArgs a = {{dq, dk, dv}, 0};
     const int pairs = dq.B * dq.Hkv * dq.slices;
     const auto grid = [&](int walks) { return (a.workgroups + 7) / 8 * 8 * walks; };
@@ -1040,17 +1029,17 @@ hipError_t launch_backward(const LinearWalkArgs &dq, const LinearWalkArgs &dk, c
     if (dq.n_segs > 1) {
         static bool raised[kMaxLdsDevices] = {};
         a.workgroups = pairs * (dq.n_segs - 1);
-        e = launch_kernel(linear_backward_kernel<M, DK, NW, true, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(1, true, false), a, stream);
+        e = launch_kernel(linear_backward_kernel<M, DK, NW, true, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(true, false), a, stream);
         if (e == hipSuccess && dq.scanned) e = launch_scan<DK, NW>(a, 2, stream);
         if (e != hipSuccess) return e;
     }
     a.workgroups = pairs * dq.n_segs;
     if (dv_alike) {
         static bool raised[kMaxLdsDevices] = {};
-        return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 3>, raised, grid(3), SH::NT, SH::lds_bytes(PIECES, false, true), a, stream);
+        return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 3>, raised, grid(3), SH::NT, SH::lds_bytes(false, true), a, stream);
     }
     static bool raised[kMaxLdsDevices] = {};
-    return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(PIECES, false, true), a, stream);
+    return launch_kernel(linear_backward_kernel<M, DK, NW, false, GROUPED, 2>, raised, grid(2), SH::NT, SH::lds_bytes(false, true), a, stream);
 }
 template <class M, int DK>
 hipError_t launch_backward_dk(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream)
@@ -1063,12 +1052,11 @@ hipError_t launch_backward_dk(const LinearWalkArgs &dq, const LinearWalkArgs &dk
 template <class M, int DK>
 hipError_t launch_values_dk(const LinearWalkArgs &a, hipStream_t stream)
 {
-    constexpr int PIECES = M::BF16 ? 2 : 1, VW = M::BF16 ? 3 : 1;
     const bool narrow = a.dv <= 64;
-    if (a.n_src > 1) return narrow ? launch_one<M, DK, 4, PIECES, VW, false, kSources, true>(a, stream)
-                                  : launch_one<M, DK, 8, PIECES, VW, false, kSources, true>(a, stream);
-    return narrow ? launch_one<M, DK, 4, PIECES, VW, false, kOne, true>(a, stream)
-                                  : launch_one<M, DK, 8, PIECES, VW, false, kOne, true>(a, stream);
+    if (a.n_src > 1) return narrow ? launch_one<M, DK, 4, false, kSources, true>(a, stream)
+                                  : launch_one<M, DK, 8, false, kSources, true>(a, stream);
+    return narrow ? launch_one<M, DK, 4, false, kOne, true>(a, stream)
+                                  : launch_one<M, DK, 8, false, kOne, true>(a, stream);
 }
 
 }  // namespace linear
