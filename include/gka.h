@@ -397,11 +397,14 @@ gka_status gka_linear_forward(const gka_linear_params *p,
  *     dgamma_t = <dS_t, S_{t-1}>,   dS_init = gamma_0 dS_0 (summed over the sequences that share a state).
  *   dq, dk, dv  io_dtype, packed like q, k, v (written; dk and dv summed over the query heads of a group)
  *   dgate       float32 like gate (written; [H_kv] with gate_per_head: summed over sequences and tokens). Formed as
- *               (<dS_final,S_T> + sum_{s>=t} (q_s . dq_s - k_s . dk_s)) / gamma_t; where a gate wipes the state it is
- *               written as 0 and the sum restarts (an infinity or NaN in a row spoils the sum of all tokens before)
+ *               (<dS_final,S_T> + sum_{s>=t} (q_s . dq_s - k_s . dk_s)) / gamma_t; for the tokens of a chunk (64, float32
+ *               tensors 32, counted from the first) that holds a gate below 1/16 from the states around the chunk, without
+ *               the division. Where a gate wipes the state it is written as 0 and the sum restarts (an infinity or NaN in a row
+ *               spoils the sum of all tokens before)
  *   dS_init     [B/share,H_kv,d_v,d_k] float32, written if not NULL; a buffer of its own (GKA_ERR_SHAPE)
  *   Nothing is added up by atomics: results are the same on every run.
- *   workspace: gka_linear_backward_workspace_bytes(p) bytes, 256-byte aligned. */
+ *   workspace: gka_linear_backward_workspace_bytes(p) bytes, 256-byte aligned: most of it two float32 states, padded to 64, 128 or
+ *   256 features, for each chunk and kv head (d = 128, bf16 tensors: 2 KiB a token), written where a chunk holds a gate below 1/16. */
 size_t gka_linear_backward_workspace_bytes(const gka_linear_params *p);
 gka_status gka_linear_backward(const gka_linear_params *p,
                                const void *q, const void *k, const void *v, const float *gate,

@@ -12,7 +12,7 @@ SOURCES = ["gka_api.hip", "gka_state_pass.hip", "gka_chunk_solve.hip", "gka_solv
            "gka_linear_bf16_256.hip", "gka_linear_f32_64.hip", "gka_linear_f32_128.hip", "gka_linear_f32_256.hip",
            "gka_linear_backward_bf16_64.hip", "gka_linear_backward_bf16_128.hip", "gka_linear_backward_bf16_256.hip",
            "gka_linear_backward_f32_64.hip", "gka_linear_backward_f32_128.hip", "gka_linear_backward_f32_256.hip",
-           "gka_linear_gradient.hip", "gka_linear_decode.hip"]
+           "gka_linear_gradient.hip", "gka_linear_small_gates.hip", "gka_linear_decode.hip"]
 # Host code of the boundary: argument validation, launch plans, workspace carving.
 API_SOURCES = ["gka_api.hip", "gka_linear_api.hip"]
 HIPCC_FLAGS = [

@@ -11,13 +11,19 @@ struct RowTensor {
     int64_t sb, st, sh;
 };
 
+// Gates up to exp(-100) (to float32's last bits there) wipe the state. Small ones are those that the gradient of the decays is not divided
+// by (gka_linear_gradient.hip).
+constexpr float kWipingGate = 3.8e-44f, kSmallGate = 0.0625f;
+__device__ __forceinline__ bool small_gate(float gate) { return gate > kWipingGate && gate < kSmallGate; }
+
 // One walk over whole sequences: y_t = S_t q_t, S_t = gate_t S_{t-1} + sum over the sources v_t k_t^T, with S [dv, dk].
 // With other tensors in the roles of q, k, v it is the forward pass and each of the three gradients (the tensors' own names
 // on the right):
 //   y   q -> q   k -> k   v -> v    forwards           dq  q -> dy  k -> v   v -> k    forwards, S transposed
 //   dv  q -> k   k -> q   v -> dy   reverse            dk  q -> v   k -> dy  v -> q    reverse, S transposed
 // A state belongs to one of the H_kv heads; n_q queries or n_src sources of a token share it (one of the two is 1).
-// reverse: token tau of the walk is token T - 1 - tau of the tensors and its gate that of token T - tau (tau = 0: 1).
+// reverse: from the last token to the first, the gate of a token being that of the one behind it (of the last: 1). The chunks are the
+// same, counted from the first token.
 struct LinearWalkArgs {
     RowTensor q, k, v;            // heads: H_kv n_q, H_kv n_src, H_kv n_src; features dk, dk, dv
     RowTensor y;                  // H_kv n_q heads, dv features (written)
@@ -35,6 +41,10 @@ struct LinearWalkArgs {
     double *dot_out;
     const float *state_dot_with;  // [B, H_kv, dv, dk]: state_dot_out [slices, B, H_kv] = its product with the last state
     double *state_dot_out;
+    // ... and at small gates, with dot_out: the state before each chunk that holds one (in the order of seg_states, with chunks from the
+    // front in the segments' place), and by the forward walk [B, H_kv, chunks] which ones those are
+    float *chunk_states;
+    int *small_gates;
     // plan
     int n_segs, seg_chunks;       // segments of the walk, chunks each
     int scanned;                  // a launch between turns what the segments add into the states that they start from (else each
@@ -76,7 +86,7 @@ hipError_t launch_linear_forward_f32_256(const LinearWalkArgs &a, hipStream_t st
 hipError_t launch_linear_values_f32_256(const LinearWalkArgs &a, hipStream_t stream);
 hipError_t launch_linear_backward_f32_256(const LinearWalkArgs &dq, const LinearWalkArgs &dk, const LinearWalkArgs &dv, bool dv_alike, hipStream_t stream);
 
-// dgate_t = ([state_dot] + sum_{s >= t} (q . dq - k . dk)) / gate_t, and the sum of gradients at shared initial states.
+// The gradient of the decays, and the sum of gradients at shared initial states.
 struct LinearGateArgs {
     const double *q_dq;           // [q_slices, B, H_kv, G, T]
     const double *k_dk;           // [k_slices, B, H_kv, T]
@@ -86,11 +96,19 @@ struct LinearGateArgs {
     float *dgate;                 // [B, T, H_kv], or [H_kv] with gate_per_head
     int gate_per_head;
     int B, T, Hkv;
+    // chunks with small gates
+    RowTensor q, k, v, dy;
+    int dk, dv, chunk;            // features; tokens of a chunk
+    const int *small_gates;       // [B, H_kv, chunks]
+    const float *S_chunk, *dS_chunk;   // [B, H_kv, slices, chunks] states: before the chunk's first token, dS behind its last one
+    int state_slice, state_dk;    // of those: k-features of a slice (of all d_k), padded d_v
     double *part_sums, *per_part; // (carved from the workspace by the launcher)
+    double *chunk_first, *per_chunk;
     int *part_open;
 };
-size_t linear_gate_workspace_bytes(int64_t pairs, int T);
-hipError_t launch_linear_gate(const LinearGateArgs &a, void *workspace, hipStream_t stream);
+size_t linear_gate_workspace_bytes(int64_t pairs, int T, int chunk);
+hipError_t launch_linear_small_gates(const LinearGateArgs &a, bool bf16, hipStream_t stream);
+hipError_t launch_linear_gate(const LinearGateArgs &a, bool bf16, void *workspace, hipStream_t stream);
 hipError_t launch_linear_state_sum(const float *per_sequence, float *out, int groups, int share, int64_t state_floats,
                                    hipStream_t stream);
 

@@ -187,7 +187,7 @@ gka::LinearWalkArgs walk_args(const gka_linear_params *p, const Sizes &s, const 
 struct BackwardPlan {
     Sizes s;
     WalkPlan q, k, v;                  // the walks of dq, dk, dv
-    size_t off_q, off_k, off_q_dot, off_k_dot, off_state_dot, off_gate, off_states, total;
+    size_t off_q, off_k, off_q_dot, off_k_dot, off_state_dot, off_gate, off_states, off_S_chunk, off_dS_chunk, off_small, total;
 };
 
 gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
@@ -209,7 +209,12 @@ gka_status plan_backward(const gka_linear_params *p, BackwardPlan *b)
     b->off_q_dot = off; off += align_up(b->q.shape.slices * tokens * b->s.G * sizeof(double), 256);
     b->off_k_dot = off; off += align_up(b->k.shape.slices * tokens * sizeof(double), 256);
     b->off_state_dot = off; off += align_up(b->q.shape.slices * b->s.pairs * sizeof(double), 256);
-    b->off_gate = off; off += align_up(gka::linear_gate_workspace_bytes(b->s.pairs, p->T), 256);
+    b->off_gate = off; off += align_up(gka::linear_gate_workspace_bytes(b->s.pairs, p->T, b->q.shape.chunk), 256);
+    // (two states for each chunk: which ones hold small gates, the host does not know)
+    const size_t chunks = (size_t)b->s.pairs * (((int64_t)p->T + b->q.shape.chunk - 1) / b->q.shape.chunk);
+    b->off_S_chunk = off; off += chunks * b->q.shape.slices * b->q.shape.state_floats * sizeof(float);
+    b->off_dS_chunk = off; off += chunks * b->q.shape.slices * b->q.shape.state_floats * sizeof(float);
+    b->off_small = off; off += align_up(chunks * sizeof(int), 256);
     b->off_states = off;
     // (room for a state of every sequence whether or not initial states are shared: one size for all calls)
     off += align_up((size_t)b->s.pairs * p->d_k * p->d_v * sizeof(float), 256);
@@ -333,6 +338,7 @@ gka_status gka_linear_backward(const gka_linear_params *p, const void *q, const 
     wq.n_q = s.G;
     wq.init = S_init; wq.share = s.share; wq.transposed = 1;
     wq.dot_with = at(q, s.q); wq.dot_out = q_dot;
+    wq.chunk_states = (float *)(ws + b.off_S_chunk); wq.small_gates = (int *)(ws + b.off_small);
     if (dS_final) {
         wq.state_dot_with = dS_final;
         wq.state_dot_out = state_dot;
@@ -344,6 +350,7 @@ gka_status gka_linear_backward(const gka_linear_params *p, const void *q, const 
     wk.reverse = 1;
     wk.init = dS_final; wk.transposed = 1;
     wk.dot_with = at(k, s.k); wk.dot_out = k_dot;
+    wk.chunk_states = (float *)(ws + b.off_dS_chunk);
     // dv_t = dS_t k_t
     gka::LinearWalkArgs wv = walk_args(p, s, b.v, gate, p->d_k, p->d_v, ws + b.off_k);
     wv.q = at(k, s.k); wv.k = at(q, s.q); wv.v = at(dy, s.o); wv.y = at(dv, packed_v);
@@ -361,7 +368,11 @@ gka_status gka_linear_backward(const gka_linear_params *p, const void *q, const 
     g.q_slices = b.q.shape.slices; g.k_slices = b.k.shape.slices; g.G = s.G;
     g.gate = gate; g.dgate = dgate; g.gate_per_head = p->gate_per_head;
     g.B = p->B; g.T = p->T; g.Hkv = p->H_kv;
-    return gka::launch_linear_gate(g, ws + b.off_gate, stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
+    g.q = wq.dot_with; g.k = wk.dot_with; g.v = wk.q; g.dy = wq.q;
+    g.dk = p->d_k; g.dv = p->d_v; g.chunk = b.q.shape.chunk;
+    g.small_gates = wq.small_gates; g.S_chunk = wq.chunk_states; g.dS_chunk = wk.chunk_states;
+    g.state_slice = b.q.shape.slice; g.state_dk = b.q.shape.padded_dk;
+    return gka::launch_linear_gate(g, s.bf16, ws + b.off_gate, stream) == hipSuccess ? GKA_OK : GKA_ERR_LAUNCH;
 }
 
 gka_status gka_linear_decode(const gka_linear_params *p, const float *S_in, float *S_out, const void *q, const void *k, const void *v,

@@ -6,14 +6,18 @@
 namespace gka {
 namespace {
 
-// dL/dlog(gate_t) is what the tokens from t on read of the states before t:
-//   L_t = x_t + L_{t+1},  x_t = sum_g q_t . dq_t - k_t . dk_t,  L_T = <dS_final, S_T>;   dgate_t = L_t / gate_t.
-// A gate of at most exp(-100) wipes the state (L_t = 0 there): the sum starts anew before it and its own gradient is
-// written as 0. A workgroup takes up to 4096 tokens of a (sequence, kv head), four consecutive ones to a thread, joined by a scan over
+// The gradient of a gate is <dS_t, S_{t-1}>. Times the gate it is what the tokens from t on read of the states before t,
+//   gate_t dgate_t = L_t = x_t + L_{t+1},  x_t = sum_g q_t . dq_t - k_t . dk_t,  L_T = <dS_final, S_T>,
+// a sum over numbers that the walks leave anyhow. But it is a difference of terms of any size whose error, float32's, L_t / gate_t
+// multiplies: a gate of 1e-8 would get 182 for a derivative of 6.1. So this form serves gates from kSmallGate = 2^-4 on (and its error
+// grows 16 times at most); the tokens of a chunk that holds a smaller one, which no error may be divided by, get the inner
+// product from the states around the chunk (gka_linear_small_gates.hip), and the sum of L starts anew before it with theirs.
+// A gate of at most exp(-100) wipes the state: its own gradient is written as 0, and L_t is 0 there.
+//
+// L: a workgroup takes up to 4096 tokens of a (sequence, kv head), four consecutive ones to a thread, joined by a scan over
 // the threads in float64; of longer sequences a first launch (SUMS) leaves what each part adds up to. 64 heads x 4096 tokens: 13 us for
 // 6 MiB, bound by the latency of one chain (gates and results of a head lie H_kv apart).
 constexpr int kThreads = 1024, kRun = 4, kPart = kThreads * kRun;
-constexpr float kWiped = 3.8e-44f;                 // exp(-100) to float32's last bits there
 
 template <bool SUMS>
 __global__ __launch_bounds__(kThreads) void linear_gate_kernel(LinearGateArgs a)
@@ -26,6 +30,9 @@ __global__ __launch_bounds__(kThreads) void linear_gate_kernel(LinearGateArgs a)
     const int b = pair / a.Hkv, h = pair % a.Hkv;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int t0 = part * kPart + tid * kRun;
+    // (a thread's tokens lie in one chunk)
+    const int64_t chunk = (int64_t)pair * ((a.T + a.chunk - 1) / a.chunk) + min(t0, a.T - 1) / a.chunk;
+    const bool small = t0 < a.T && a.small_gates[chunk] != 0;
     // (tokens behind the last one read it again, so that all reads are under way at once, and are then left out)
     float gate[kRun];
     double x[kRun];
@@ -54,10 +61,14 @@ __global__ __launch_bounds__(kThreads) void linear_gate_kernel(LinearGateArgs a)
 #pragma unroll
     for (int i = kRun - 1; i >= 0; --i) {
         sum += x[i];
-        if (!(gate[i] > kWiped)) {
+        if (!(gate[i] > kWipingGate)) {
             sum = 0.0;
             open = 0;
         }
+    }
+    if (small) {
+        sum = t0 % a.chunk == 0 ? a.chunk_first[chunk] : 0.0;
+        open = 0;
     }
     // this thread's run with those of the threads behind it in the wave
 #pragma unroll
@@ -104,10 +115,10 @@ __global__ __launch_bounds__(kThreads) void linear_gate_kernel(LinearGateArgs a)
 #pragma unroll
     for (int i = kRun - 1; i >= 0; --i) {
         const int t = t0 + i;
-        if (t >= a.T) continue;
+        if (t >= a.T || small) continue;
         c += x[i];
         double d = c / (double)gate[i];
-        if (!(gate[i] > kWiped)) c = d = 0.0;
+        if (!(gate[i] > kWipingGate)) c = d = 0.0;
         if (!a.gate_per_head) a.dgate[((int64_t)b * a.T + t) * a.Hkv + h] = (float)d;
         total += d;
     }
@@ -130,9 +141,13 @@ __global__ __launch_bounds__(64) void linear_gate_heads_kernel(LinearGateArgs a)
     const int h = blockIdx.x * 64 + threadIdx.x;
     if (h >= a.Hkv) return;
     const int parts = (a.T + kPart - 1) / kPart;
+    const int chunks = (a.T + a.chunk - 1) / a.chunk;
+    const bool small = small_gate(a.gate[h]);      // (of all chunks)
+    const int n = small ? chunks : parts;
+    const double *from = small ? a.per_chunk : a.per_part;
     double x = 0.0;
     for (int b = 0; b < a.B; ++b)
-        for (int i = 0; i < parts; ++i) x += a.per_part[((int64_t)b * a.Hkv + h) * parts + i];
+        for (int i = 0; i < n; ++i) x += from[((int64_t)b * a.Hkv + h) * n + i];
     a.dgate[h] = (float)x;
 }
 
@@ -149,21 +164,24 @@ __global__ __launch_bounds__(256) void linear_state_sum_kernel(const float *per_
 
 }  // namespace
 
-size_t linear_gate_workspace_bytes(int64_t pairs, int T)
+size_t linear_gate_workspace_bytes(int64_t pairs, int T, int chunk)
 {
-    const int64_t parts = ((int64_t)T + kPart - 1) / kPart;
-    return (size_t)(pairs * parts) * (2 * sizeof(double) + sizeof(int));
+    const int64_t parts = ((int64_t)T + kPart - 1) / kPart, chunks = ((int64_t)T + chunk - 1) / chunk;
+    return (size_t)(pairs * parts) * (2 * sizeof(double) + sizeof(int)) + (size_t)(pairs * chunks) * 2 * sizeof(double);
 }
 
-hipError_t launch_linear_gate(const LinearGateArgs &a0, void *workspace, hipStream_t stream)
+hipError_t launch_linear_gate(const LinearGateArgs &a0, bool bf16, void *workspace, hipStream_t stream)
 {
     LinearGateArgs a = a0;
-    const int64_t pairs = (int64_t)a.B * a.Hkv, parts = ((int64_t)a.T + kPart - 1) / kPart;
+    const int64_t pairs = (int64_t)a.B * a.Hkv, parts = ((int64_t)a.T + kPart - 1) / kPart, chunks = ((int64_t)a.T + a.chunk - 1) / a.chunk;
     if (pairs * parts > 0x7fffffff) return hipErrorInvalidValue;
     a.part_sums = (double *)workspace;
     a.per_part = a.part_sums + pairs * parts;
-    a.part_open = (int *)(a.per_part + pairs * parts);
-    hipError_t e;
+    a.chunk_first = a.per_part + pairs * parts;
+    a.per_chunk = a.chunk_first + pairs * chunks;
+    a.part_open = (int *)(a.per_chunk + pairs * chunks);
+    hipError_t e = launch_linear_small_gates(a, bf16, stream);
+    if (e != hipSuccess) return e;
     if (parts > 1) {
         hipLaunchKernelGGL(linear_gate_kernel<true>, dim3((unsigned)(pairs * parts)), dim3(kThreads), 0, stream, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;

@@ -351,27 +351,29 @@ struct StateAt {
 
 // The rows of one head chunk by chunk, each chunk's a raw buffer: reads of tokens and features that do not exist give zeros and writes
 // to them are dropped by the buffer's bounds, without a branch. `lane` offsets (chunk_offset below) count from the first row of
-// the buffer. Rows are below 2^23 elements apart, so that a chunk's bytes stay below 2^30.
+// the buffer. Rows are below 2^23 elements apart, so that a chunk's bytes stay below 2^30. Both directions have the same chunks, of C
+// tokens counted from the first one: in reverse it is the walk's first chunk whose rows may be fewer, those that it meets last.
 template <int C, int ES>
 struct ChunkRows {
-    const char *base;                              // lowest row of a whole chunk (of the last one it may lie before the tensor)
+    const char *base;                              // the chunk's lowest token
     int pitch;                                     // bytes
-    __device__ __forceinline__ ChunkRows(const RowTensor &x, int b, int head, int chunk, int T, int reverse)
+    // chunk: from the front
+    __device__ __forceinline__ ChunkRows(const RowTensor &x, int b, int head, int chunk)
     {
         pitch = (int)x.st * ES;
-        base = (const char *)x.p + (b * x.sb + head * x.sh) * ES + (int64_t)(reverse ? T - C - chunk * C : chunk * C) * pitch;
+        base = (const char *)x.p + (b * x.sb + head * x.sh) * ES + (int64_t)chunk * C * pitch;
     }
     __device__ __forceinline__ void next(int reverse) { base += (int64_t)(reverse ? -C : C) * pitch; }
     // count: tokens of the chunk (0: an empty buffer); head: bytes to a further head
-    __device__ __forceinline__ buffer_rsrc rows(int count, int reverse, int64_t head = 0) const
+    __device__ __forceinline__ buffer_rsrc rows(int count, int64_t head = 0) const
     {
-        return __builtin_amdgcn_make_buffer_rsrc((void *)(base + head + (reverse ? (C - count) * pitch : 0)), 0, count * pitch, 0x00020000);
+        return __builtin_amdgcn_make_buffer_rsrc((void *)(base + head), 0, count * pitch, 0x00020000);
     }
-    // byte offset of the walk's first token of the chunk
-    __device__ __forceinline__ int top(int count, int reverse) const { return reverse ? (count - 1) * pitch : 0; }
+    // byte offset of the walk's first token of a whole chunk
+    __device__ __forceinline__ int top(int reverse) const { return reverse ? (C - 1) * pitch : 0; }
 };
 // Offset of feature `col` of the chunk's row `row` but for ChunkRows::top(); far outside for a feature that does not exist. A token
-// behind the last one lies behind the buffer's end or, in reverse, at a negative offset, which counts as one of 2^31 or more.
+// behind the last one lies behind the buffer's end.
 template <int ES>
 __device__ __forceinline__ int chunk_offset(const RowTensor &x, int row, int col, bool exists, int reverse)
 {
@@ -421,7 +423,7 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     constexpr int LOOKAHEAD = ROOMY ? 4 : GROUP == kSources ? 1 : 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char *sK = smem, *sV = smem + SH::k_bytes;
-    float *tables = (float *)(sV + SH::v_bytes);   // [2][5][64]: log2 decay (two floats), weight in the state, zeta of a token (both with the state's factor); that factor
+    float *tables = (float *)(sV + SH::v_bytes);   // [2][5][64]: log2 decay (two floats), weight in the state, zeta of a token (both with the state's factor); see decays
     unsigned char *sQ = (unsigned char *)tables + SH::tables, *sP = sQ + SH::q_bytes;
     double *sDot = (double *)(sP + SH::p_bytes);        // [NW][C]: the waves' parts of the dot products (DOT)
 
@@ -434,6 +436,9 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     const int seg = workgroup / n_pairs / a.slices;
     const int b = pair / a.Hkv, h = pair % a.Hkv;
     const int n_chunks = (a.T + C - 1) / C;
+    // chunk c of the walk is chunk `from_front(c)` of the tensors; the last of those has `last_count` tokens
+    const auto from_front = [&](int c) { return a.reverse ? n_chunks - 1 - c : c; };
+    const int last_count = a.T - (n_chunks - 1) * C;
     const int chunk_begin = seg * a.seg_chunks;
     const int chunk_end = min(chunk_begin + a.seg_chunks, n_chunks);
     const int steps = GROUP == kQueries ? a.n_q : GROUP == kSources ? a.n_src : 1;
@@ -452,13 +457,13 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     // (chunks behind the segment: an empty buffer, zeros without a read. Every path writes the registers, so that they are not
     // held from where they are staged to where the next rows are asked for.)
     typedef ChunkRows<C, ES> Tokens;
-    Tokens q_rows(a.q, b, h * (GROUP == kQueries ? steps : 1), chunk_begin, a.T, a.reverse);
-    Tokens k_rows(a.k, b, h * (GROUP == kSources ? steps : 1), chunk_begin, a.T, a.reverse);
-    Tokens v_rows(a.v, b, h * (GROUP == kSources ? steps : 1), chunk_begin, a.T, a.reverse);
-    auto count_of = [&](int c) { return c < chunk_end ? min(C, a.T - c * C) : 0; };
+    Tokens q_rows(a.q, b, h * (GROUP == kQueries ? steps : 1), from_front(chunk_begin));
+    Tokens k_rows(a.k, b, h * (GROUP == kSources ? steps : 1), from_front(chunk_begin));
+    Tokens v_rows(a.v, b, h * (GROUP == kSources ? steps : 1), from_front(chunk_begin));
+    auto count_of = [&](int c) { return c >= chunk_end ? 0 : from_front(c) == n_chunks - 1 ? last_count : C; };
     auto fetch_rows = [&](auto &to, const Tokens &x, int64_t head, int count, int offset, int rows_per) {
-        const buffer_rsrc rows = x.rows(count, a.reverse, head);
-        const int top = x.top(count, a.reverse), step = (a.reverse ? -rows_per : rows_per) * x.pitch;
+        const buffer_rsrc rows = x.rows(count, head);
+        const int top = x.top(a.reverse), step = (a.reverse ? -rows_per : rows_per) * x.pitch;
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(to) / 16); ++i)
             to[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, offset + (top + i * step), 0, 0));
@@ -508,27 +513,29 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     const int v_lane = VT::further(col_place<M, VT>(lane), w * (16 * ES / 16));
 
     // ---- decays: the last wave leaves those of the next chunk in the tables, lane j those of token j. The state is kept up to a
-    // factor, `scale`, which takes up the chunks' decays; only where it gets small are the registers multiplied by it (table[256];
-    // 1: not in this chunk), instead of all of them in every chunk.
+    // factor, `scale`, which takes up the chunks' decays; only where it gets small are the registers multiplied by it, instead of all
+    // of them in every chunk. Table[256]: by what they are multiplied in this chunk (1: not), [257] the factor behind the chunk, [258]
+    // before it, [259] (DOT) whether the chunk holds a small gate.
     float gate = 1.0f, seg_decay = 1.0f, scale = 1.0f;
+    uint64_t small_gates = 0;                      // tokens of the chunk whose decays were formed last that have one
     auto fetch_gate = [&](int c) {
-        const int tau = c * C + lane;
+        const int token = a.reverse ? (n_chunks - c) * C - lane : c * C + lane;       // whose gate it is (reverse: of the one behind)
         gate = 1.0f;
-        if (lane < C && tau < a.T && !(a.reverse && tau == 0))
-            gate = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + (a.reverse ? a.T - tau : tau)) * a.Hkv + h];
+        if (lane < C && token >= 0 && token < a.T) gate = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + token) * a.Hkv + h];
     };
     auto decays = [&](int c) {
         const double G = wave_inclusive_scan_f64(log2_gate_f64(gate)), total = lane63_f64(G);
         const float hi = (float)G, zeta_C = __builtin_amdgcn_exp2f((float)total);
-        const float after = scale * zeta_C;
+        if constexpr (DOT) small_gates = __ballot(small_gate(gate));
+        const float before = scale, after = scale * zeta_C;
         const bool small = after < 0x1p-16f;
         float *t = tables + (c & 1) * 320 + lane;
         t[0] = hi;
         t[64] = (float)(G - (double)hi);
-        t[128] = c * C + lane < a.T ? __builtin_amdgcn_exp2f((float)(total - G)) * (small ? 1.0f : 1.0f / after) : 0.0f;
+        t[128] = __builtin_amdgcn_exp2f((float)(total - G)) * (small ? 1.0f : 1.0f / after);
         t[192] = __builtin_amdgcn_exp2f(hi) * scale;
         scale = small ? 1.0f : after;
-        t[256] = lane == 0 ? (small ? after : 1.0f) : scale;
+        t[256] = lane == 0 ? (small ? after : 1.0f) : lane == 2 ? before : scale;
         seg_decay *= zeta_C;
     };
 
@@ -573,16 +580,16 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     // dot products of chunk c (query s), whose parts lie in LDS since the step before: the same barriers serve both. A wave without decays
     // and with the fewest masked products does this.
     auto add_dots = [&](int c, int s) {
-        const int lane = anew(lane0), tau = c * C + lane;
-        if (w != NW - 2 || lane >= C || tau >= a.T) return;
+        const int lane = anew(lane0), token = from_front(c) * C + (a.reverse ? C - 1 - lane : lane);
+        if (w != NW - 2 || lane >= C || token >= a.T) return;
         double dot = 0.0;
 #pragma unroll
         for (int i = 0; i < NW; ++i) dot += sDot[i * C + lane];
-        a.dot_out[(((int64_t)slice * n_pairs + pair) * a.n_q + s) * a.T + (a.reverse ? a.T - 1 - tau : tau)] = dot;
+        a.dot_out[(((int64_t)slice * n_pairs + pair) * a.n_q + s) * a.T + token] = dot;
     };
 
-    Tokens y_rows(a.y, b, h * (GROUP == kQueries ? steps : 1), chunk_begin, a.T, a.reverse);
-    Tokens dot_rows(a.dot_with, b, h * (GROUP == kQueries ? steps : 1), chunk_begin, a.T, a.reverse);
+    Tokens y_rows(a.y, b, h * (GROUP == kQueries ? steps : 1), from_front(chunk_begin));
+    Tokens dot_rows(a.dot_with, b, h * (GROUP == kQueries ? steps : 1), from_front(chunk_begin));
     if (w == NW - 1) {
         decays(chunk_begin);
         fetch_gate(chunk_begin + 1);
@@ -610,9 +617,19 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
             if (SUMMARY || ROOMY) fetch_next();
             lds_barrier();                         // (no wait for the rows in flight)
             __builtin_amdgcn_sched_barrier(0);
-            if (w == NW - 1 && s == 0 && c + 1 < chunk_end) {
-                decays(c + 1);                     // (its gates were asked for a chunk ago)
-                fetch_gate(c + 2);
+            if (w == NW - 1 && s == 0) {
+                if constexpr (DOT) {
+                    // (in reverse the gate of the chunk's first token is the first one of the walk's next chunk)
+                    const bool any = a.reverse ? (small_gates & ~1ull) != 0 || (__ballot(small_gate(gate)) & 1) != 0 : small_gates != 0;
+                    if (lane == 0) {
+                        tables[(c & 1) * 320 + 259] = any ? 1.0f : 0.0f;
+                        if (!a.reverse && slice == 0) a.small_gates[(int64_t)pair * n_chunks + c] = any;
+                    }
+                }
+                if (c + 1 < chunk_end) {
+                    decays(c + 1);                 // (its gates were asked for a chunk ago)
+                    fetch_gate(c + 2);
+                }
             }
 
             if constexpr (!SUMMARY) {
@@ -718,8 +735,8 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                 if constexpr (DOT) {
                     if (GROUP == kQueries || s + 1 == steps) {
                         const int lane = anew(lane0), n = lane & 15, kg = lane >> 4;
-                        const buffer_rsrc with = dot_rows.rows(count, a.reverse, (GROUP == kQueries ? s : 0) * a.dot_with.sh * ES);
-                        const int top = dot_rows.top(count, a.reverse);
+                        const buffer_rsrc with = dot_rows.rows(count, (GROUP == kQueries ? s : 0) * a.dot_with.sh * ES);
+                        const int top = dot_rows.top(a.reverse);
 #pragma unroll
                         for (int tb = 0; tb < TB; ++tb) {
                             const int at = chunk_offset<ES>(a.dot_with, 16 * tb + n, v0 + 16 * w + 4 * kg, v0 + 16 * w < a.dv, a.reverse) + top;
@@ -783,8 +800,8 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                             if (kg == 0) sDot[w * C + 16 * tb + n] = dot;
                         }
                     }
-                    const buffer_rsrc out = y_rows.rows(count, a.reverse, to_head * a.y.sh * ES);
-                    const int out_top = y_rows.top(count, a.reverse);
+                    const buffer_rsrc out = y_rows.rows(count, to_head * a.y.sh * ES);
+                    const int out_top = y_rows.top(a.reverse);
                     if constexpr (BF16) {
                         // (lanes of neighbouring kg exchange runs of two token blocks, so that a lane stores eight features at once)
 #pragma unroll
@@ -814,6 +831,16 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
 
             // ---- S <- zeta_C S + sum_s w_s v_s k_s^T
             if (GROUP == kSources ? s == 0 : s + 1 == steps) {
+                if constexpr (DOT) {
+                    // (the state before the chunk, for the gradients of its small gates)
+                    if (__builtin_amdgcn_readfirstlane(__float_as_uint(sHi[259])) != 0) {
+                        const float before = sHi[258];
+                        const int64_t at = (((int64_t)pair * a.slices + slice) * n_chunks + from_front(c)) * state_floats;
+                        float *to = a.chunk_states + at + (w * NJ * 64 + anew(lane0)) * 4;
+#pragma unroll
+                        for (int j = 0; j < NJ; ++j) *(f32x4 *)(to + j * 256) = acc[j] * before;
+                    }
+                }
                 const float factor = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(sHi[256])));
                 if (factor != 1.0f) {
 #pragma unroll
