@@ -350,8 +350,9 @@ gka_status gka_forward_sketched(const gka_params *p,
  * Tensors of rows: q [B,T,H,d_k], k [B,T,H_kv,d_k], v [B,T,H_kv,d_v], o [B,T,H,d_v], all GKA_F32 or all GKA_BF16, 16-byte
  * aligned; each has element strides of its own. Sums, states and decays are float32 or wider for either type; with bf16
  * tensors what is computed in float32 enters the matrix products as three bf16 pieces, all of its bits, so that an output carries
- * the rounding of its own type. An infinity or NaN in a row of q, k or v reaches the outputs that depend on the row and no others
- * (rows of a padded batch behind a sequence's end may hold anything); where it reaches, NaN may stand for an infinity.
+ * the rounding of its own type. An infinity or NaN in a row of q, k or v, or in a state, reaches the outputs that depend on it and no
+ * others (rows of a padded batch behind a sequence's end may hold anything, and nothing crosses a gate that wipes the state); where
+ * it reaches, NaN may stand for an infinity.
  *
  * Limits: B H_kv < 2^21, B H <= 2^26, T and cache_tokens <= 2^31 - 2^13 (GKA_ERR_SHAPE beyond). Tensors that a call writes overlap
  * none that it reads, and their rows not each other, unless it is said below. */

@@ -52,7 +52,7 @@ struct LinearWalkArgs {
     int slices;                   // of dv, a workgroup takes one
     float *seg_states;            // [B, H_kv, slices, n_segs, slice, DK] in the kernel's order: what each segment adds, then the
                                   // state that it starts from
-    float *seg_decay;             // [B, H_kv, n_segs]
+    float *seg_decay;             // [B, H_kv, n_segs]; negative: wiped
     int seg_turned[3];            // not 0: seg_states are those of the walk with transposed states: its waves, tiles a wave, slices
 };
 

@@ -68,7 +68,14 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a, 
         if (tid < count) sg[tid] = a.gate_per_head ? a.gate[h] : a.gate[((int64_t)b * a.T + t0 + tid) * a.Hkv + h];
         __syncthreads();
         for (int t = 0; t < count; ++t) {
-            const float gate = sg[t];
+            float gate = sg[t];
+            if (!(gate > kWipingGate)) {           // (nothing of the state before comes through, whatever it holds)
+                gate = 0.0f;
+#pragma unroll
+                for (int i = 0; i < NR; ++i)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) S[i][j] = zero;
+            }
             float x[NR];
 #pragma unroll
             for (int i = 0; i < NR; ++i) x[i] = sv[t * RP * NR + i * RP + tid / LPR];
@@ -263,13 +270,18 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
         };
         constexpr int MOST = HEADS == 1 ? 16 : 8, FLY = LR < MOST ? LR : MOST;    // reads in flight
         double behind = 0.0;                       // log2 decay over the tokens behind the tile
-        for (int j0 = len / 64 * 64; j0 >= 0; j0 -= 64) {
+        bool wiped = false;                        // nothing before that tile comes through
+        for (int j0 = len / 64 * 64; j0 >= 0 && !wiped; j0 -= 64) {
             const int count = len + 1 - j0 < 64 ? len + 1 - j0 : 64;
             double lg = 0.0;
+            bool wipes = false;
             if (lane < count) {
                 const float gate = a.gate_per_head || j0 + lane == len ? gate_new : a.gate_cache[cache_row + (int64_t)(j0 + lane) * a.Hkv];
                 lg = log2_gate_f64(gate);
+                wipes = !(gate > kWipingGate);
             }
+            const uint64_t wiping = __ballot(wipes);
+            const int first = wiping != 0 ? 63 - __builtin_clzll(wiping) : 0;        // the first token of the tile that counts
             for (int s0 = 0; s0 < count; s0 += FLY * RP) {
                 piece p[FLY];
 #pragma unroll
@@ -291,17 +303,21 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
                 }
             }
             const double G = wave_inclusive_scan_f64(lg), total = lane63_f64(G);
-            const float weight = lane < count ? __builtin_amdgcn_exp2f((float)(behind + (total - G))) : 0.0f;
+            const bool counts = lane >= first && lane < count;
+            const float weight = counts ? __builtin_amdgcn_exp2f((float)(behind + (total - G))) : 0.0f;
             behind += total;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the wave's own scores)
 #pragma unroll
             for (int g = 0; g < HEADS; ++g)
-                if (g < m) score[g * 64 + lane] = lane < count ? score[g * 64 + lane] * weight : 0.0f;
+                if (g < m) score[g * 64 + lane] = counts ? score[g * 64 + lane] * weight : 0.0f;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             for (int s0 = 0; s0 < count; s0 += FLY * RP) {
                 piece p[FLY];
 #pragma unroll
-                for (int i = 0; i < FLY; ++i) p[i] = fetch(vc, vc_step, v_new, j0 + s0 + i * RP + r, v_in && s0 + i * RP + r < count);
+                for (int i = 0; i < FLY; ++i) {
+                    const int token = s0 + i * RP + r;
+                    p[i] = fetch(vc, vc_step, v_new, j0 + token, v_in && token >= first && token < count);
+                }
 #pragma unroll
                 for (int i = 0; i < FLY; ++i) {
                     float x[E];
@@ -317,8 +333,9 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
                 }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (read before the next tile's are written)
+            wiped = wiping != 0;
         }
-        const float zeta = __builtin_amdgcn_exp2f((float)behind);
+        const float zeta = wiped ? 0.0f : __builtin_amdgcn_exp2f((float)behind);
 #pragma unroll
         for (int g = 0; g < HEADS; ++g) {
             if (g >= m) continue;
@@ -330,9 +347,10 @@ __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(Linear
                 elem_t *out = const_cast<elem_t *>(row_of(a.y, b, h * a.G + head0 + g)) + E * l;
                 const float *s = sY + (c + g) * ys + E * l;
 #pragma unroll
-                for (int e = 0; e < E; e += 4)
-                    IO::store4(out, e, zeta * s[e] + y[g][e], zeta * s[e + 1] + y[g][e + 1], zeta * s[e + 2] + y[g][e + 2],
-                               zeta * s[e + 3] + y[g][e + 3]);
+                for (int e = 0; e < E; e += 4) {
+                    const f32x4 x = wiped ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : *(const f32x4 *)(s + e);
+                    IO::store4(out, e, zeta * x[0] + y[g][e], zeta * x[1] + y[g][e + 1], zeta * x[2] + y[g][e + 2], zeta * x[3] + y[g][e + 3]);
+                }
             }
         }
         c += m;

@@ -193,10 +193,9 @@ __device__ __forceinline__ void cut(const float *x, typename M::frag (&f)[N])
     }
 }
 
-// A wave's v fragments with zeros for infinities and NaN. Returns the first token of the chunk that has one in feature lane % 16 (any
-// number above them all: none), or -1 in all lanes if none of the wave's features has.
+// Whether a wave's v fragments hold infinities or NaN.
 template <class M, int SB>
-__device__ __forceinline__ int without_nonfinite(typename M::frag (&v)[SB][M::STEPS], int lane)
+__device__ __forceinline__ bool any_nonfinite(const typename M::frag (&v)[SB][M::STEPS])
 {
     // (0 unless one of them is infinite or NaN)
     float zero = 0.0f;
@@ -216,8 +215,14 @@ __device__ __forceinline__ int without_nonfinite(typename M::frag (&v)[SB][M::ST
                 zero = __builtin_fmaf(v[sb][st], 0.0f, zero);
             }
         }
-    if (__builtin_expect(__ballot(!(zero == 0.0f)) == 0, 1)) return -1;
-    int first = 1 << 20;
+    return __ballot(!(zero == 0.0f)) != 0;
+}
+
+// The fragments with zeros for infinities and NaN; returns the chunk's tokens that have one in feature lane % 16, a bit each.
+template <class M, int SB>
+__device__ __forceinline__ uint64_t clear_nonfinite(typename M::frag (&v)[SB][M::STEPS], int lane)
+{
+    uint64_t bad = 0;
 #pragma unroll
     for (int sb = 0; sb < SB; ++sb)
 #pragma unroll
@@ -225,22 +230,48 @@ __device__ __forceinline__ int without_nonfinite(typename M::frag (&v)[SB][M::ST
             if constexpr (M::BF16) {
                 u32x4_t u = __builtin_bit_cast(u32x4_t, v[sb][st]);
 #pragma unroll
-                for (int e = 7; e >= 0; --e) {
+                for (int e = 0; e < 8; ++e) {
                     const uint32_t exponent = e & 1 ? 0x7f800000u : 0x7f80u;
                     if ((u[e / 2] & exponent) == exponent) {
-                        first = min(first, 32 * sb + 16 * (e >> 2) + (e & 3) + 4 * (lane >> 4));
+                        bad |= 1ull << (32 * sb + 16 * (e >> 2) + (e & 3) + 4 * (lane >> 4));
                         u[e / 2] &= e & 1 ? 0xffffu : 0xffff0000u;
                     }
                 }
                 v[sb][st] = __builtin_bit_cast(typename M::frag, u);
             } else if ((__float_as_uint(v[sb][st]) & 0x7f800000u) == 0x7f800000u) {
-                first = min(first, 32 * sb + 16 * (st >> 2) + (st & 3) + 4 * (lane >> 4));
+                bad |= 1ull << (32 * sb + 16 * (st >> 2) + (st & 3) + 4 * (lane >> 4));
                 v[sb][st] = 0.0f;
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-    first = min(first, __shfl_xor(first, 16, 64));
-    return min(first, __shfl_xor(first, 32, 64));
+#pragma unroll
+    for (int lanes = 16; lanes <= 32; lanes *= 2) {
+        const uint32_t lo = __shfl_xor((uint32_t)bad, lanes, 64), hi = __shfl_xor((uint32_t)(bad >> 32), lanes, 64);
+        bad |= (uint64_t)hi << 32 | lo;
+    }
+    return bad;
+}
+
+// The fragments with zeros for the tokens before `first`.
+template <class M, int SB>
+__device__ __forceinline__ void clear_before(typename M::frag (&v)[SB][M::STEPS], int first, int lane)
+{
+#pragma unroll
+    for (int sb = 0; sb < SB; ++sb)
+#pragma unroll
+        for (int st = 0; st < M::STEPS; ++st) {
+            const int token = 32 * sb + 4 * (lane >> 4);
+            if constexpr (M::BF16) {
+                u32x4_t u = __builtin_bit_cast(u32x4_t, v[sb][st]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (token + 16 * (e >> 2) + (e & 3) < first) u[e / 2] &= e & 1 ? 0xffffu : 0xffff0000u;
+                v[sb][st] = __builtin_bit_cast(typename M::frag, u);
+            } else if (token + 16 * (st >> 2) + (st & 3) < first) {
+                v[sb][st] = 0.0f;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
 }
 
 // DK: padded features of q and k. NW: waves, 16 features of v each.
@@ -515,7 +546,8 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     // ---- decays: the last wave leaves those of the next chunk in the tables, lane j those of token j. The state is kept up to a
     // factor, `scale`, which takes up the chunks' decays; only where it gets small are the registers multiplied by it, instead of all
     // of them in every chunk. Table[256]: by what they are multiplied in this chunk (1: not), [257] the factor behind the chunk, [258]
-    // before it, [259] (DOT) whether the chunk holds a small gate.
+    // before it, [259] (DOT) whether the chunk holds a small gate, [260], [261] its tokens whose gates wipe the state, a bit each: what
+    // lies before the last of those is left out by selections, in the few chunks that hold one, so that nothing of it comes through.
     float gate = 1.0f, seg_decay = 1.0f, scale = 1.0f;
     uint64_t small_gates = 0;                      // tokens of the chunk whose decays were formed last that have one
     auto fetch_gate = [&](int c) {
@@ -526,17 +558,18 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     auto decays = [&](int c) {
         const double G = wave_inclusive_scan_f64(log2_gate_f64(gate)), total = lane63_f64(G);
         const float hi = (float)G, zeta_C = __builtin_amdgcn_exp2f((float)total);
+        const uint64_t wiping = __ballot(!(gate > kWipingGate));
         if constexpr (DOT) small_gates = __ballot(small_gate(gate));
         const float before = scale, after = scale * zeta_C;
-        const bool small = after < 0x1p-16f;
+        const bool small = wiping != 0 || after < 0x1p-16f;
         float *t = tables + (c & 1) * 320 + lane;
         t[0] = hi;
         t[64] = (float)(G - (double)hi);
         t[128] = __builtin_amdgcn_exp2f((float)(total - G)) * (small ? 1.0f : 1.0f / after);
         t[192] = __builtin_amdgcn_exp2f(hi) * scale;
         scale = small ? 1.0f : after;
-        t[256] = lane == 0 ? (small ? after : 1.0f) : lane == 2 ? before : scale;
-        seg_decay *= zeta_C;
+        t[256] = lane == 0 ? (small ? after : 1.0f) : lane == 2 ? before : lane < 4 ? scale : __uint_as_float((uint32_t)(lane == 4 ? wiping : wiping >> 32));
+        seg_decay = wiping != 0 || seg_decay < 0.0f ? -1.0f : seg_decay * zeta_C;
     };
 
     Rows rows;
@@ -566,6 +599,10 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
             }
             for (int before = 0; before < seg; ++before) {
                 const float decay = a.seg_decay[(int64_t)pair * a.n_segs + before];
+                if (decay < 0.0f) {                // (wiped)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                }
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
                     const f32x4 adds = next[j];
@@ -597,6 +634,10 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
     for (int c = chunk_begin; c < chunk_end; ++c) {
         const float *sHi = tables + (c & 1) * 320, *sLo = sHi + 64, *sW = sHi + 128, *sZ = sHi + 192;
         const int count = count_of(c);
+        uint64_t wiping = 0;
+        auto wiping_tokens = [&] {
+            return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(__float_as_int(sHi[261])) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(__float_as_int(sHi[260]));
+        };
         f32x4 y[TB];
         for (int s = 0; s < steps; ++s) {
             lds_barrier();                         // the tiles of the step before have been read
@@ -633,6 +674,7 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
             }
 
             if constexpr (!SUMMARY) {
+                wiping = wiping_tokens();
                 // ---- masked products M[t, s] (k_s . q_t): a unit is a block of 16 tokens and 32 keys, left as operand fragments
                 const int k_at = anew(k_lane);
                 int q_at = anew(q_lane);
@@ -676,6 +718,12 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                             m[4 * half + r] = below < 0 || (below == 0 && 4 * kg + r > n) ? 0.0f : product;
                         }
                     }
+                    if (__builtin_expect(wiping != 0, 0)) {
+                        const uint64_t up_to = wiping & ((2ull << (16 * tb + n)) - 1);
+                        const int first = up_to != 0 ? 63 - __builtin_clzll(up_to) : 0;        // (the first key that the token sees)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) m[e] = 32 * sb + 16 * (e >> 2) + 4 * kg + (e & 3) < first ? 0.0f : m[e];
+                    }
 #pragma unroll
                     for (int st = 0; st < STEPS; ++st) {
                         frag f[PIECES];
@@ -718,6 +766,13 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) y[tb][r] *= zeta;
                     }
+                    if (__builtin_expect(wiping != 0, 0)) {
+                        const int seen = __builtin_ctzll(wiping);                              // (tokens that see the state)
+#pragma unroll
+                        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) y[tb][r] = 16 * tb + n < seen ? y[tb][r] : 0.0f;
+                    }
                 }
             }
             frag vt[SB][STEPS];                    // v, features on the lanes, contraction over the tokens
@@ -729,7 +784,8 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
             if constexpr (!SUMMARY) {
                 // Infinities and NaN in v reach the tokens from their own on, in their feature; a product with the zeros of the tokens before
                 // would carry them there too. They leave these products and are put in below, where there are any.
-                const int first_bad = without_nonfinite<M>(vt, lane0);
+                const bool nonfinite = any_nonfinite<M>(vt);
+                if (__builtin_expect(nonfinite, 0)) clear_nonfinite<M>(vt, lane0);
                 // (rows of the dot products: before the next chunk's, which are not waited for with them)
                 std::conditional_t<BF16, u32x2_t, u32x4_t> dot_row[DOT ? TB : 1];
                 if constexpr (DOT) {
@@ -768,13 +824,22 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                             y[tb] = M::mma(vt[sb][st], p.f[e], y[tb]);
                         }
                     });
-                if (__builtin_expect(__builtin_amdgcn_readfirstlane(first_bad) >= 0, 0)) {
+                if (__builtin_expect(nonfinite, 0)) {
                     const int lane = anew(lane0);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int from = __shfl(first_bad, 4 * (lane >> 4) + r, 64);
+                    for (int sb = 0; sb < SB; ++sb)
 #pragma unroll
-                        for (int tb = 0; tb < TB; ++tb) y[tb][r] = 16 * tb + (lane & 15) >= from ? __builtin_nanf("") : y[tb][r];
+                        for (int st = 0; st < STEPS; ++st) vt[sb][st] = col_frag<M, VT>(sV, v_lane, 0, sb, st);
+                    const uint64_t bad = clear_nonfinite<M>(vt, lane);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint64_t of_feature = (uint64_t)__shfl((uint32_t)(bad >> 32), 4 * (lane >> 4) + r, 64) << 32 | __shfl((uint32_t)bad, 4 * (lane >> 4) + r, 64);
+#pragma unroll
+                        for (int tb = 0; tb < TB; ++tb) {
+                            const uint64_t up_to = (2ull << (16 * tb + (lane & 15))) - 1, wiped = wiping & up_to;
+                            const uint64_t before = wiped != 0 ? (1ull << (63 - __builtin_clzll(wiped))) - 1 : 0;
+                            y[tb][r] = (of_feature & up_to & ~before) != 0 ? __builtin_nanf("") : y[tb][r];
+                        }
                     }
 #pragma unroll
                     for (int sb = 0; sb < SB; ++sb)
@@ -841,14 +906,26 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
                         for (int j = 0; j < NJ; ++j) *(f32x4 *)(to + j * 256) = acc[j] * before;
                     }
                 }
+                if constexpr (SUMMARY) wiping = wiping_tokens();
                 const float factor = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(sHi[256])));
-                if (factor != 1.0f) {
+                if (__builtin_expect(wiping != 0, 0)) {
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                } else if (factor != 1.0f) {
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) acc[j] *= factor;
                 }
             }
             if (GROUP == kSources || s + 1 == steps) {
                 const int kt_at = anew(kt_lane), kg = anew(lane0) >> 4;
+                if (__builtin_expect(wiping > 1, 0)) {
+                    // The tokens before the last wiping one add nothing, whatever they hold. (Every wave clears all their k rows, which no
+                    // other product of this step reads any more: what it then reads are zeros, its own or another wave's.)
+                    const int first = 63 - __builtin_clzll(wiping);
+                    clear_before<M>(vt, first, lane0);
+                    for (int i = lane0; i < first * KROW; i += 64) *(u32x4_t *)(sK + KT::at(i / KROW, i % KROW)) = u32x4_t{0, 0, 0, 0};
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                }
                 // BATCH tiles of the state at a time, the steps of the contraction over the tokens on the outside
                 constexpr int BATCH = !BF16 ? (NJ < 8 ? NJ : 8) : LOOKAHEAD, PARTS = NJ / BATCH;
                 struct Keys {
@@ -929,7 +1006,7 @@ __device__ __forceinline__ void walk(const LinearWalkArgs &a, int workgroup)
             float scale = 1.0f;
             if (a.final_times_gate) scale = a.gate_per_head ? a.gate[h] : a.gate[(int64_t)b * a.T * a.Hkv + h];
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) S.store(j, acc[j] * scale);
+            for (int j = 0; j < NJ; ++j) S.store(j, scale > kWipingGate ? acc[j] * scale : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
         }
     }
 }
@@ -992,6 +1069,7 @@ __global__ __launch_bounds__(64) void linear_scan_kernel(LinearBackwardArgs walk
         for (int i = 0; i < AHEAD; ++i) {
             if (seg + i > last) break;
             *(f32x4 *)(s + (seg + i) * state_floats) = run;
+            if (factor[i] < 0.0f) run = f32x4{0.0f, 0.0f, 0.0f, 0.0f};     // (wiped)
             run = run * factor[i] + adds[i];
         }
     }
