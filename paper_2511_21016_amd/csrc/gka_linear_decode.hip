@@ -132,12 +132,13 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearDecodeArgs a, 
 // ---- shared ----------------------------------------------------------------------------------------------------------
 // A workgroup takes up to 16 columns of one (prefix, kv head): a column is a query head of a sequence, G of them to a
 // sequence, one behind the other. First S q of its columns on the matrix cores (16 x 16 tiles: 16 rows of S to a wave; S cut into
-// three bf16 pieces, which hold all its bits, or float32), then each wave the cached tokens of its columns, up to HEADS of
-// one sequence at a time, LR lanes to a row of 16-byte pieces.
+// three bf16 pieces, which hold all its bits, or float32), then each wave the cached tokens of its columns, two at most, together
+// where they are heads of one sequence, LR lanes to a row of 16-byte pieces.
 // Bound by the latency of a wave's reads, one batch after the other: 256 samples of 4 prefixes, 32 heads of d 128, up to 128 tokens:
 // 67 us for 262 MiB (4.1 TB/s) from HBM. One head alone leaves registers for 16 reads in flight instead of 8 (72 us). Waves that take the
-// columns by falling length instead of in their order: 1 per cent, not kept.
-constexpr int kSharedCols = 16, kSharedHeads = 4, kSharedWaves = 8;
+// columns by falling length instead of in their order: 1 per cent, not kept. Two heads with room for no more than two (no wave has more): 8 heads
+// of d 64 to a state, 512 samples of 8 prefixes, 67 us; with the registers for four 102.
+constexpr int kSharedCols = 16, kSharedWaves = 8, kSharedHeads = kSharedCols / kSharedWaves;
 
 template <bool BF16, int LR, int HEADS>
 __global__ __launch_bounds__(64 * kSharedWaves) void linear_shared_kernel(LinearSharedArgs a, int ncol)
