@@ -597,7 +597,7 @@ def _workspace_bytes(plan, backward):
     if nbytes is None:
         nbytes = (linear_backward_workspace_bytes if backward else linear_forward_workspace_bytes)(plan.params)
         if nbytes == 0:                            # let the library say what is wrong with the parameters
-            _check(linear_forward_raw(plan.params, None, None, None, None, None))
+            _check(linear_backward_raw(plan.params, *[None] * 9) if backward else linear_forward_raw(plan.params, *[None] * 5))
         if backward:
             plan.backward_bytes = nbytes
         else:
