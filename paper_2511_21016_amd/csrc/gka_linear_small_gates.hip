@@ -8,17 +8,15 @@
 // source. Gates that wipe leave out what lies on their other side, whatever it is.
 //
 // The walks leave S and D of these chunks alone, in the order in which they hold them. bf16 tensors: products on the bf16 MFMA, rows as
-// they are, states in three pieces; float32: on the float32 MFMA. A workgroup looks at every gridDim-th chunk; where none has
-// small gates, the launch takes 3 us. Bound by one chunk's chain of reads, products and readers, 15 us (bf16, d 128: staging and A[u, s]
-// 3 us, the states 7, the readers 5) with one workgroup on a CU; all chunks of 64 heads x 4096 tokens: 380 us. Rows of q, k, v,
+// they are, states in three pieces; float32: on the float32 MFMA. A workgroup, one to a CU, looks at every gridDim-th chunk;
+// where none has small gates, the launch takes 4 us (1024 workgroups, four rounds of them: 12). Bound by one chunk's chain of reads, products and readers, 15 us (bf16, d 128: staging and A[u, s]
+// 3 us, the states 7, the readers 5) with one workgroup on a CU; all chunks of 64 heads x 4096 tokens: 390 us. Rows of q, k, v,
 // dy come through LDS: read where they are needed, 32 bytes of 16 rows at a time, they took three times as long.
 #include "gka_device.hpp"
 #include "gka_linear.hpp"
 
 namespace gka {
 namespace {
-
-constexpr int kSmallWorkgroups = 1024;
 
 // Features with padding, and bytes from row to row in LDS (16 more: neighbouring rows lie in other banks).
 __host__ __device__ __forceinline__ int padded_features(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
@@ -287,7 +285,7 @@ __global__ __launch_bounds__(512) void linear_small_gates_kernel(LinearGateArgs 
 hipError_t launch_linear_small_gates(const LinearGateArgs &a, bool bf16, hipStream_t stream)
 {
     const int64_t chunks = (int64_t)a.B * a.Hkv * (((int64_t)a.T + a.chunk - 1) / a.chunk);
-    const dim3 grid((unsigned)(chunks < kSmallWorkgroups ? chunks : kSmallWorkgroups));
+    const dim3 grid((unsigned)(chunks < kComputeUnits ? chunks : kComputeUnits));
     const size_t lds = (size_t)4 * a.chunk * small_gates_pitch(a, bf16 ? 2 : 4);
     static bool raised[kMaxLdsDevices] = {};
     constexpr size_t most = (size_t)4 * 64 * (256 * 2 + 16);       // (float32: 32 rows of 256 x 4 + 16 bytes, less)
