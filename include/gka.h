@@ -352,7 +352,8 @@ gka_status gka_forward_sketched(const gka_params *p,
  * tensors what is computed in float32 enters the matrix products as three bf16 pieces, all of its bits, so that an output carries
  * the rounding of its own type. An infinity or NaN in a row of q, k or v, or in a state, reaches the outputs that depend on it and no
  * others (rows of a padded batch behind a sequence's end may hold anything, and nothing crosses a gate that wipes the state); where
- * it reaches, NaN may stand for an infinity.
+ * it reaches, NaN may stand for an infinity. Whole sequences keep a state up to a factor of 2^16: numbers of 2^110 and more in v or in a
+ * state may become infinite.
  *
  * Limits: B H_kv < 2^21, B H <= 2^26, T and cache_tokens <= 2^31 - 2^13 (GKA_ERR_SHAPE beyond). Tensors that a call writes overlap
  * none that it reads, and their rows not each other, unless it is said below. */

@@ -638,9 +638,10 @@ def gka_linear_forward(q, k, v, gate, *, S_init=None, return_state=False, worksp
 
 
 def gka_linear_backward(q, k, v, gate, dy, *, S_init=None, dS_final=None, workspace=None, walk_chunks=0):
-    """gka_linear_backward on torch CUDA tensors: the arguments of gka_linear_forward, dy [B,T,H,d_v] like its output and
-    dS_final [B,H_kv,d_v,d_k] the gradient at its final states. Returns a dict: dq, dk, dv in the tensors' dtype (packed),
-    dgate float32 like gate and, with S_init, dS_init like it (summed over the sequences that share a state)."""
+    """gka_linear_backward on torch CUDA tensors: the arguments of gka_linear_forward, dy [B,T,H,d_v] like its output (one
+    with strides of 0, of an expanded scalar, is refused: dy.contiguous()) and dS_final [B,H_kv,d_v,d_k] the gradient at its final
+    states. Returns a dict: dq, dk, dv in the tensors' dtype (packed), dgate float32 like gate and, with S_init, dS_init like it
+    (summed over the sequences that share a state)."""
     import torch
     load_library()
     stream = _stream_of(q)

@@ -1086,6 +1086,6 @@ const char *gka_status_string(gka_status s)
     return "unknown status";
 }
 
-int gka_version(void) { return 900; }
+int gka_version(void) { return 901; }
 
 }  // extern "C"

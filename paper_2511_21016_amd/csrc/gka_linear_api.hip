@@ -13,8 +13,9 @@ constexpr int64_t kWalkWorkgroups = 4 * gka::kComputeUnits;
 
 // Up to this many segments a walk adds up the states of those before it by itself; above, a launch between (the scan) does. The three
 // walks of the backward pass, one of which reads the states transposed, add up 65536 floats at most, or 4 segments. Measured, us, added
-// up against scanned: forward pass, 8 states of 128 x 128, 16 segments 19.6 : 23.4; backward pass 54.6 : 41.5, 8 segments 40.8 : 38.6,
-// 16 such states, 16 segments 88 : 67; 16 states of 64 x 64, 16 segments 45.6 : 49.8; of 256 x 128, 12 segments 138 : 106, 5 81 : 83.
+// up against scanned (one chunk to a segment): forward pass, 8 states of 128 x 128, 16 segments 22.3 : 24.6; backward pass 62.8 : 47.1, 8
+// segments 40.6 : 36.8, 16 such states, 16 segments 97 : 58; 16 states of 64 x 64, 16 segments 38.3 : 41.1; 8 of 256 x 128, 12 segments
+// 98 : 62, 5 60 : 52.
 constexpr int kMostSegmentsAddedUp = 16;
 int most_added_up_backward(int64_t state_floats)
 {
@@ -108,7 +109,7 @@ struct WalkPlan {
 };
 
 // What a pass does over its chunks: `walks` walks in one launch, each chunk at walk_cost, after `summaries` in another, at summary_cost
-// (in times of a chunk of the forward pass's summary, 1.7 us at d 128).
+// (in times of a chunk of the forward pass's summary, 1.7 us at d 128). The costs are those of bf16 tensors at d 128.
 struct PassCost {
     int walks, summaries, most_added_up;
     float walk_cost, summary_cost;
@@ -120,8 +121,9 @@ PassCost backward_cost(int G, int64_t state_floats) { return {3, 2, most_added_u
 // whether one or two workgroups share it, so a launch takes ceil(workgroups / 256) segments' times, and the most segments for each
 // such number are the candidates; the summaries walk all segments but the last once more; starting workgroups, the launches and adding
 // up the states before a segment, or the scan, cost the rest. Measured, us, by chunks of a segment: 64 states
-// x 4096 tokens, forward pass 8: 96, 16: 98, 32: 196, backward pass 8: 346, 16: 327; 8 states x 4 heads x 32768 tokens 8: 249, 16: 258,
-// 32: 640; backward pass of 8 states x 3 heads x 1337 tokens 1: 77, 2: 81, 3: 103; float32, 16 states x 1001 tokens 1: 44, 2: 28, 4: 37.
+// x 4096 tokens, forward pass 4: 138, 8: 115, 16: 115, 32: 199, backward pass 8: 371, 16: 334, 32: 384; 8 states x 4 heads x 32768 tokens
+// 8: 277, 16: 296, 32: 523; backward pass of 8 states x 3 heads x 1337 tokens 1: 71, 2: 82, 3: 110; float32, 16 states x 1001 tokens
+// 1: 37, 2: 29, 4: 38.
 int walk_segment(int64_t states, int64_t chunks, const PassCost &c)
 {
     const auto rounds = [](int64_t workgroups) { return (float)((workgroups + gka::kComputeUnits - 1) / gka::kComputeUnits); };

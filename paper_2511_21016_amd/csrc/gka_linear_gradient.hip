@@ -15,7 +15,7 @@ namespace {
 // A gate of at most exp(-100) wipes the state: its own gradient is written as 0, and L_t is 0 there.
 //
 // L: a workgroup takes up to 4096 tokens of a (sequence, kv head), four consecutive ones to a thread, joined by a scan over
-// the threads in float64; of longer sequences a first launch (SUMS) leaves what each part adds up to. 64 heads x 4096 tokens: 13 us for
+// the threads in float64; of longer sequences a first launch (SUMS) leaves what each part adds up to. 64 heads x 4096 tokens: 14 us for
 // 6 MiB, bound by the latency of one chain (gates and results of a head lie H_kv apart).
 constexpr int kThreads = 1024, kRun = 4, kPart = kThreads * kRun;
 

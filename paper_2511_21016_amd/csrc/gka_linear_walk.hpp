@@ -13,11 +13,10 @@
 // (128: four waves on a SIMD) matter more here than operand reuse: a chunk is a chain of short phases with barriers between.
 // Segments start from states that a summary launch (SUMMARY: the updates alone) leaves in the workspace.
 //
-// Bound by the phases of a chunk, with two workgroups on a CU to fill each other's waits: 64 states of d 128 x 4096 tokens (bf16), walk 73
-// us, summary 29 us (120 MiB of reads, 4.3 TB/s); of the walk 58 us remain without its traffic and 58 without its products, 33
-// without both; its matrix pipe is busy 33 per cent of the time, vector instructions take 48, LDS 40 (1/6 of that bank conflicts). The
-// backward pass's three walks: 283 us, 37, 52 and 36 per cent. Slices of 64 features with four waves: 109 us the pass instead of 99; tiles of
-// 32 features a wave would need 256 registers, two waves on a SIMD.
+// Bound by the phases of a chunk, with two workgroups on a CU to fill each other's waits: 64 states of d 128 x 4096 tokens (bf16), walk 86
+// us, summary 34 us (120 MiB of reads, 3.7 TB/s); the walk's matrix pipe is busy 39 per cent of the time, vector instructions take 51,
+// LDS 36 (1/7 of that bank conflicts). The backward pass's three walks: 290 us, 37, 54 and 35 per cent. Slices of 64 features with four
+// waves took 10 per cent more for the pass; tiles of 32 features a wave would need 256 registers, two waves on a SIMD.
 //
 // Precision. bf16 tensors enter the products as they are; what is computed in float32 (states, masked products, weighted
 // v) is cut into three bf16 pieces, which hold all of its 24 bits. (Two pieces in the readout round one in 400 of the bf16 outputs
